@@ -242,12 +242,81 @@ int kv_append(int model, int batch, const void *k_new, const void *v_new, const 
 int kv_append_chunk(int model, int batch, const void *k_new, const void *v_new, const int32_t *q_lens,
                     const int32_t *ctx_lens);
 
+/* ---- from a layer's projections into the cache ----------------------------- */
+
+/* Rotary positions.  Elements 0 .. rot_dim - 1 of a head form rot_dim / 2 pairs; pair i turns by
+ * inv_freq[i] radians a token, (a, b) -> magnitude * (a cos - b sin, b cos + a sin), and the
+ * elements from rot_dim on stay as they are.  PKV_ROTARY_HALF: pair i is elements i and
+ * i + rot_dim / 2; PKV_ROTARY_PAIRS: elements 2 i and 2 i + 1.  Angles are exact to 2^-32 of a
+ * circle at every int32 position (the frequencies are kept as 64-bit fractions of a circle).
+ * rotary_create takes the frequencies (HOST double [rot_dim / 2], finite, rot_dim even, 2 .. 128),
+ * so any rule of scaling them can be used; it returns an id (lowest unused, 0 .. 63) that any
+ * model and layer may use, PKV_E_NOMEM beyond.  rotary_destroy waits for the device; graphs
+ * captured with the id must not be replayed afterwards.
+ * rotary_frequencies is a host call (no device work): inv_freq[i] = f_i = base^(-2 i / rot_dim), by
+ * `scaling` changed for contexts `factor` times those of training; returns rot_dim / 2.
+ *   PKV_ROTARY_PLAIN   not changed (factor, trained, low and high are not looked at)
+ *   PKV_ROTARY_LINEAR  f_i / factor: positions are squeezed
+ *   PKV_ROTARY_BASE    base * factor^(rot_dim / (rot_dim - 2)) instead of base: the slowest pair
+ *                      is squeezed by factor, the fastest not at all
+ *   PKV_ROTARY_RAMP    by the turns n_i = trained * f_i / 2 pi that a pair makes over a trained context:
+ *                      f_i / factor for n_i <= low, f_i for n_i >= high, in proportion between */
+enum { PKV_ROTARY_HALF = 0, PKV_ROTARY_PAIRS = 1 };
+enum { PKV_ROTARY_PLAIN = 0, PKV_ROTARY_LINEAR = 1, PKV_ROTARY_BASE = 2, PKV_ROTARY_RAMP = 3 };
+int rotary_frequencies(int rot_dim, double base, int scaling, double factor, double trained, double low,
+                       double high, double *inv_freq);
+int rotary_create(int rot_dim, int layout, const double *inv_freq, double magnitude);
+int rotary_destroy(int rotary);
+
+/* New tokens on their way from a layer's projections to its attention, in one launch: queries and
+ * keys are normed head by head and rotated to their positions, queries go to q_out, keys and values
+ * into the cache.  Per head x of head_dim elements, in fp32: y = x / sqrt(mean(x^2) + eps) * weight
+ * where there is a weight, then the rotation, then one rounding to bf16 (to nearest even).  Keys so
+ * rounded, and values as they came, go into the cache exactly as kv_append / kv_append_chunk would put them
+ * there, scales and codes of e4m3 models included.
+ *   q, k, v     dev, bf16; a token's q_heads (kv_heads) heads of head_dim elements lie side by side,
+ *               and tokens are *_stride elements apart (0: packed), so all three may be parts of
+ *               one fused projection.  16-byte aligned rows are read faster; any alignment works.
+ *   q_weight, k_weight   dev, bf16 [head_dim], or NULL: that one is not normed
+ *   rotary      an id of rotary_create with rot_dim <= head_dim (PKV_E_SHAPE), or -1: no rotation
+ *   before      dev int32 [batch], or NULL (zeros): tokens in front of the row's first one, e.g. those
+ *               of a shared prefix: token j of row s stands at position before[s] + j
+ *   q_out       dev, bf16 [tokens][q_heads][head_dim], 16-byte aligned, as the attention calls read it.
+ *               May be q itself if q is packed; must not overlap the inputs otherwise.
+ * ctx_lens, q_lens, the order of the tokens, return values and errors are those of kv_append and
+ * kv_append_chunk.  A row whose context length is refused (bit 1 of pkv_device_errors()) gets no
+ * K and V; its queries are written all the same.  Enqueues only. */
+typedef struct pkv_qkv {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const void *q_weight, *k_weight;
+    float eps;
+    int rotary;
+    const int32_t *before;
+} pkv_qkv;
+int qkv_append(int model, int batch, const pkv_qkv *in, const int32_t *ctx_lens, void *q_out);
+int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens,
+                     void *q_out);
+
 /* Tokens [tok_begin, tok_begin + n_tok) of a sequence back in the logical layout of
  * kv_write: k_out, v_out dev [n_tok][kv_heads][head_dim] (bf16 values or e4m3 codes);
  * e4m3 only: k_scale_out, v_scale_out dev fp32 [n_tok][kv_heads], the scale of the
  * block each token lives in.  For tests and debugging.  Enqueues only. */
 int kv_read(int model, int seq, int tok_begin, int n_tok, void *k_out, void *v_out,
             float *k_scale_out, float *v_scale_out);
+
+/* Cached tokens of several sequences as packed bf16 rows, the way back of kv_append_chunk (a sequence
+ * is swapped out, its cache handed to another GPU, or the tokens behind the last whole block of a
+ * prefix copied to a sequence that shares the rest).  Entry i < n takes tokens tok_begin[i] ..
+ * tok_begin[i] + n_tok[i] - 1 of sequence seqs[i]; the entries' rows follow each other in k_out and v_out
+ * (dev, bf16 [sum n_tok][kv_heads][head_dim], 16-byte aligned).  bf16 models: the values as stored;
+ * e4m3 models: decode(code) * scale, in fp32, rounded to bf16 once (to nearest even).  seqs, tok_begin,
+ * n_tok: HOST int32 [n], n <= 4096; a sequence may come more than once.  Tokens in reserved blocks that
+ * nothing was written to come as whatever is there.  Returns sum n_tok; PKV_E_RANGE beyond a row's blocks
+ * or 2^24 tokens.  Enqueues only, except that after enqueue-only bookkeeping calls it first waits
+ * for them, as kv_write does. */
+int kv_gather(int model, int n, const int32_t *seqs, const int32_t *tok_begin, const int32_t *n_tok, void *k_out,
+              void *v_out);
 
 /* ---- decode attention (Background: paged attention over the block table) -- */
 

@@ -10,6 +10,15 @@ import os
 import numpy as np
 
 PKV_BF16, PKV_E4M3 = 0, 1
+ROTARY_HALF, ROTARY_PAIRS = 0, 1
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class _Qkv(C.Structure):
+    """pkv_qkv"""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rotary", C.c_int),
+                ("before", C.c_void_p)]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -70,6 +79,12 @@ def _load():
         "kv_append": (i, [i, i, vp, vp, vp]),
         "kv_append_chunk": (i, [i, i, vp, vp, vp, vp]),
         "kv_read": (i, [i, i, i, i, vp, vp, vp, vp]),
+        "kv_gather": (i, [i, i, vp, vp, vp, vp, vp]),
+        "rotary_frequencies": (i, [i, C.c_double, i, C.c_double, C.c_double, C.c_double, C.c_double, vp]),
+        "rotary_create": (i, [i, i, vp, C.c_double]),
+        "rotary_destroy": (i, [i]),
+        "qkv_append": (i, [i, i, vp, vp, vp]),
+        "qkv_append_chunk": (i, [i, i, vp, vp, vp, vp]),
         "model_set_batch": (i, [i, i, i]),
         "decode_attention": (i, [i, vp, vp, vp, vp]),
         "decode_attention_ex": (i, [i, i, vp, vp, i, vp, vp]),
@@ -99,7 +114,8 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
            "seq_release", "seq_release_batch", "balloon_resize_enqueue", "seq_reserve_batch_enqueue", "seq_release_batch_enqueue",
            "pkv_ticket_result", "model_block_table", "kv_write", "kv_append", "kv_append_chunk", "kv_read", "model_set_batch", "decode_attention",
            "decode_attention_ex", "decode_attention_static", "decode_attention_multi", "prefill_attention", "pool_export_state", "pool_stats",
-           "arbitrate_requests", "place_models"]
+           "arbitrate_requests", "place_models", "rotary_frequencies", "rotary_create", "rotary_destroy", "qkv_append", "qkv_append_chunk",
+           "kv_gather"]
 
 
 def _f64(a):
@@ -130,6 +146,17 @@ def place_models(n_gpus, capacity, tau, token_rate, token_size, slo, weight, cur
     if rc < 0:
         raise ValueError(f"place_models: {rc}")
     return out[:t.size].tolist()
+
+
+def rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, trained=1.0, low=1.0, high=4.0, lib=None):
+    """Host-only call (needs no GPU): -> the frequencies that rotary_create takes, float64 [rot_dim / 2]."""
+    lib = lib or _load()
+    out = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
+    rc = lib.rotary_frequencies(int(rot_dim), float(base), ROTARY_SCALINGS[scaling], float(factor), float(trained), float(low), float(high),
+                                out.ctypes.data_as(C.c_void_p))
+    if rc < 0:
+        raise ValueError(f"rotary_frequencies: {rc}")
+    return out
 
 
 class PrismKV:
@@ -362,6 +389,40 @@ class PrismKV:
         self.torch.cuda.current_stream(self.device).synchronize()
         return rc
 
+    # ---- from a layer's projections into the cache
+    def rotary_frequencies(self, *args, **kw):
+        return rotary_frequencies(*args, lib=self.lib, **kw)
+
+    def rotary_create(self, rot_dim, layout, inv_freq, magnitude=1.0):
+        f = _f64(inv_freq)
+        assert f.size == rot_dim // 2
+        return self.lib.rotary_create(int(rot_dim), int(layout), f.ctypes.data_as(C.c_void_p), float(magnitude))
+
+    def rotary_destroy(self, rotary):
+        return self.lib.rotary_destroy(rotary)
+
+    def _qkv(self, model, q, k, v, q_weight, k_weight, eps, rotary, before):
+        hq, hkv, d, _ = self._shape[model]
+        strides = []
+        for x, heads in ((q, hq), (k, hkv), (v, hkv)):
+            # a token's heads side by side, tokens any distance apart
+            assert x.dim() == 3 and tuple(x.shape[1:]) == (heads, d) and x.element_size() == 2
+            assert x.stride(2) == 1 and (heads == 1 or x.stride(1) == d)
+            strides.append(x.stride(0) if x.shape[0] > 1 else 0)
+        a = lambda t: None if t is None else t.data_ptr()
+        return _Qkv(a(q), a(k), a(v), *strides, a(q_weight), a(k_weight), eps, rotary, a(before))
+
+    def qkv_append_dev(self, model, q, k, v, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
+        """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues."""
+        x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
+        return self.lib.qkv_append(model, ctx_lens.numel(), C.byref(x), self._p(ctx_lens), self._p(q_out))
+
+    def qkv_append_chunk_dev(self, model, q, k, v, q_lens, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
+        """The same for packed chunks; q_lens: host int32 numpy array.  Only enqueues."""
+        q_lens = np.ascontiguousarray(q_lens, dtype=np.int32)
+        x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
+        return self.lib.qkv_append_chunk(model, q_lens.size, C.byref(x), q_lens.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(q_out))
+
     def kv_read(self, model, seq, tok_begin, n_tok):
         """-> (code, k, v, k_scale, v_scale) as numpy: elements [n_tok][Hkv][D], scales [n_tok][Hkv] (None for bf16)."""
         t = self.torch
@@ -379,6 +440,12 @@ class PrismKV:
         if dtype == 0:
             kn, vn = kn.view(np.uint16), vn.view(np.uint16)
         return rc, kn, vn, (None if ks is None else ks.cpu().numpy()), (None if vs is None else vs.cpu().numpy())
+
+    def kv_gather_dev(self, model, seqs, tok_begin, n_tok, k_out, v_out):
+        """Lists or host int32 arrays; k_out, v_out: device tensors, bf16 [sum n_tok][Hkv][D].  Only enqueues."""
+        lists = [np.ascontiguousarray(x, dtype=np.int32) for x in (seqs, tok_begin, n_tok)]
+        assert lists[0].size == lists[1].size == lists[2].size
+        return self.lib.kv_gather(model, lists[0].size, *[x.ctypes.data_as(C.c_void_p) for x in lists], self._p(k_out), self._p(v_out))
 
     def model_set_batch(self, model, batch, row_stride):
         return self.lib.model_set_batch(model, batch, row_stride)

@@ -247,6 +247,23 @@ int64_t wait_ticket(int slot) {
     return r == kPending ? (int64_t)PKV_E_INTERNAL : r;
 }
 
+// A rotation (rotary_create): its pairs' turns per token, in device memory.
+struct Rotary {
+    uint64_t *turns = nullptr;
+    int rot_dim = 0, layout = 0;
+    float magnitude = 1.f;
+};
+Rotary g_rotary[PKV_MAX_ROTARY];
+constexpr int64_t kQueryWaves = 4096;     // waves for queries that a launch of qkv_append_chunk has at least, where there are as many
+
+// An angle as a fraction of a circle, in 2^-64 of one: |radians| / 2 pi modulo 1, to the 53 bits of the quotient.
+uint64_t circle_fraction(double radians) {
+    double whole;
+    const double f = modf(fabs(radians) * 0.15915494309189533577, &whole);
+    const uint64_t x = f >= 1.0 ? 0 : (uint64_t)ldexp(f, 64);
+    return radians < 0.0 ? 0 - x : x;
+}
+
 void free_model_dev(Model &m) {
     (void)hipFree(m.dev.frames); (void)hipFree(m.dev.bits); (void)hipFree(m.dev.mark); (void)hipFree(m.dev.rows);
     (void)hipFree(m.dev.row_len); (void)hipFree(m.dev.counters);
@@ -1615,8 +1632,8 @@ struct PlanBuilder {
     uint32_t units[PKV_PLAN_SEQS];
     uint64_t order[PKV_PLAN_SEQS];               // length above; below, the earlier of equals first
     bool in_order = true;
-    explicit PlanBuilder(int batch) {
-        const int launches = (batch + PKV_PLAN_SEQS - 1) / PKV_PLAN_SEQS;
+    explicit PlanBuilder(int batch, int most = PKV_PLAN_SEQS) {
+        const int launches = (batch + most - 1) / most;
         per_launch = (batch + launches - 1) / launches;
         p.n_seqs = p.seq0 = 0;
     }
@@ -1647,6 +1664,42 @@ struct PlanBuilder {
         return done;
     }
 };
+
+int kv_gather(int model, int n, const int32_t *seqs, const int32_t *tok_begin, const int32_t *n_tok, void *k_out, void *v_out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (n < 0 || n > PKV_MAX_SEQS) return PKV_E_RANGE;
+    if (n == 0) return 0;
+    if (!seqs || !tok_begin || !n_tok || !k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return PKV_E_ARG;
+    if (m->stale) {                 // the range checks below need the rows' true lengths
+        const int rcs = reconcile_pool(m->pool);
+        if (rcs) return rcs;
+    }
+    const int T = g_pools[m->pool].T;
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (seqs[i] < 0 || seqs[i] >= m->dev.max_seqs || tok_begin[i] < 0 || n_tok[i] < 0) return PKV_E_ARG;
+        if (n_tok[i] > 0 && ((int64_t)tok_begin[i] + n_tok[i] + T - 1) / T > m->row_len[seqs[i]]) return PKV_E_RANGE;
+        total += n_tok[i];
+        if (total > (int64_t)1 << 24) return PKV_E_RANGE;
+    }
+    AttnDesc d{};
+    fill_addressing(d, *m);
+    GatherPlan g;
+    PlanBuilder plan(n, PKV_PLAN_FEW);
+    for (int i = 0; i < n; ++i) {
+        if (plan.full()) {
+            g.rows = few_of(plan.take(i));
+            HIP_TRY(pkv_launch_kv_gather(d, g, k_out, v_out, g_stream));
+        }
+        g.at[plan.p.n_seqs].seq = seqs[i];
+        g.at[plan.p.n_seqs].begin = tok_begin[i];
+        plan.add((uint32_t)n_tok[i], n_tok[i] > 0 ? (uint32_t)((tok_begin[i] + n_tok[i] - 1) / T - tok_begin[i] / T + 1) : 0u, 0u, 0u);
+    }
+    g.rows = few_of(plan.take(n));
+    HIP_TRY(pkv_launch_kv_gather(d, g, k_out, v_out, g_stream));
+    return (int)total;
+}
 
 int kv_append_chunk(int model, int batch, const void *k_new, const void *v_new, const int32_t *q_lens,
                     const int32_t *ctx_lens) {
@@ -1694,6 +1747,156 @@ int kv_append(int model, int batch, const void *k_new, const void *v_new, const 
 }
 
 /* -------------------------------------------------------- decode attention */
+
+/* ------------------------------------------------ norm, rotate and append */
+
+int rotary_frequencies(int rot_dim, double base, int scaling, double factor, double trained, double low, double high, double *inv_freq) {
+    if (rot_dim < 2 || (rot_dim & 1) || rot_dim > 128 || !inv_freq || !(base > 0.0) || !isfinite(base)) return PKV_E_ARG;
+    if (scaling < PKV_ROTARY_PLAIN || scaling > PKV_ROTARY_RAMP) return PKV_E_ARG;
+    if (scaling != PKV_ROTARY_PLAIN && !(factor > 0.0 && isfinite(factor))) return PKV_E_ARG;
+    if (scaling == PKV_ROTARY_RAMP && !(trained > 0.0 && isfinite(trained) && low < high && isfinite(low) && isfinite(high))) return PKV_E_ARG;
+    if (scaling == PKV_ROTARY_BASE) {
+        if (rot_dim < 4) return PKV_E_ARG;                 // one pair, of frequency 1 whatever the base
+        base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    }
+    const int n = rot_dim / 2;
+    for (int i = 0; i < n; ++i) {
+        double f = pow(base, -(double)i / n);
+        if (scaling == PKV_ROTARY_LINEAR) f /= factor;
+        if (scaling == PKV_ROTARY_RAMP) {
+            double keep = (trained * f * 0.15915494309189533577 - low) / (high - low);
+            keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        inv_freq[i] = f;
+    }
+    return n;
+}
+
+int rotary_create(int rot_dim, int layout, const double *inv_freq, double magnitude) {
+    if (rot_dim < 2 || (rot_dim & 1) || rot_dim > 128 || !inv_freq) return PKV_E_ARG;
+    if (layout != PKV_ROTARY_HALF && layout != PKV_ROTARY_PAIRS) return PKV_E_ARG;
+    if (!isfinite(magnitude) || !isfinite((float)magnitude)) return PKV_E_ARG;
+    uint64_t turns[64];
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        if (!isfinite(inv_freq[i])) return PKV_E_ARG;
+        turns[i] = circle_fraction(inv_freq[i]);
+    }
+    int id = -1;
+    for (int i = 0; i < PKV_MAX_ROTARY && id < 0; ++i)
+        if (!g_rotary[i].turns) id = i;
+    if (id < 0) return PKV_E_NOMEM;
+    uint64_t *dev = nullptr;
+    HIP_TRY(hipMalloc((void **)&dev, sizeof turns));
+    const hipError_t e = hipMemcpy(dev, turns, sizeof(uint64_t) * (rot_dim / 2), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+        (void)hipFree(dev);
+        return fail_hip(e, "rotary_create");
+    }
+    g_rotary[id] = Rotary{dev, rot_dim, layout, (float)magnitude};
+    return id;
+}
+
+int rotary_destroy(int rotary) {
+    if (rotary < 0 || rotary >= PKV_MAX_ROTARY || !g_rotary[rotary].turns) return PKV_E_HANDLE;
+    HIP_TRY(hipDeviceSynchronize());
+    (void)hipFree(g_rotary[rotary].turns);
+    g_rotary[rotary] = Rotary{};
+    return PKV_OK;
+}
+
+// What the two appends check and lay out alike.  Returns PKV_OK or an error code.
+static int fill_qkv(QkvArgs &a, const Model &m, const pkv_qkv &in, void *q_out) {
+    if (!in.q || !in.k || !in.v || !q_out) return PKV_E_ARG;
+    if (((uintptr_t)q_out & 15) || (((uintptr_t)in.q | (uintptr_t)in.k | (uintptr_t)in.v | (uintptr_t)in.q_weight | (uintptr_t)in.k_weight) & 1)) return PKV_E_ARG;
+    if ((in.q_weight || in.k_weight) && !(in.eps >= 0.f && isfinite(in.eps))) return PKV_E_ARG;
+    a.q = (const uint16_t *)in.q;
+    a.k = (const uint16_t *)in.k;
+    a.v = (const uint16_t *)in.v;
+    const int64_t q_row = (int64_t)m.Hq * m.D, kv_row = (int64_t)m.Hkv * m.D;
+    a.q_stride = in.q_stride ? in.q_stride : q_row;
+    a.k_stride = in.k_stride ? in.k_stride : kv_row;
+    a.v_stride = in.v_stride ? in.v_stride : kv_row;
+    if (a.q_stride < q_row || a.k_stride < kv_row || a.v_stride < kv_row) return PKV_E_ARG;
+    a.q_out = (uint16_t *)q_out;
+    a.q_weight = (const uint16_t *)in.q_weight;
+    a.k_weight = (const uint16_t *)in.k_weight;
+    a.eps = in.eps;
+    a.before = in.before;
+    a.turns = nullptr;
+    a.rot = a.pairs = 0;
+    a.magnitude = 1.f;
+    if (in.rotary != -1) {
+        if (in.rotary < 0 || in.rotary >= PKV_MAX_ROTARY || !g_rotary[in.rotary].turns) return PKV_E_HANDLE;
+        const Rotary &r = g_rotary[in.rotary];
+        if (r.rot_dim > m.D) return PKV_E_SHAPE;
+        a.turns = r.turns;
+        a.rot = r.rot_dim;
+        a.pairs = r.layout == PKV_ROTARY_PAIRS;
+        a.magnitude = r.magnitude;
+    }
+    a.q_aligned = ((uintptr_t)in.q & 15) == 0 && a.q_stride % 8 == 0;
+    return PKV_OK;
+}
+
+// Query heads of a token per wave: few tokens come a wave for every 512 elements, many a wave each (its angles are worked out once).
+static int wave_heads_for(const Model &m, int64_t tokens) {
+    const int at_once = 512 / m.D, turns = (m.Hq + at_once - 1) / at_once;
+    int64_t n = turns * tokens / kQueryWaves;
+    n = n < 1 ? 1 : (n > turns ? turns : n);
+    return (int)n * at_once;
+}
+
+int qkv_append(int model, int batch, const pkv_qkv *in, const int32_t *ctx_lens, void *q_out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return 0;
+    if (!in || !ctx_lens) return PKV_E_ARG;
+    QkvArgs a{};
+    const int rc = fill_qkv(a, *m, *in, q_out);
+    if (rc) return rc;
+    a.wave_heads = wave_heads_for(*m, batch);
+    AttnDesc d{};
+    fill_addressing(d, *m);
+    d.batch = batch;
+    d.ctx_lens = ctx_lens;
+    HIP_TRY(pkv_launch_qkv_append(d, a, g_stream));
+    return batch;
+}
+
+int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, void *q_out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return 0;
+    if (!in || !q_lens || !ctx_lens) return PKV_E_ARG;
+    int64_t total = 0;
+    for (int s = 0; s < batch; ++s) {
+        if (q_lens[s] < 0) return PKV_E_ARG;
+        total += q_lens[s];
+        if (total > (int64_t)1 << 24) return PKV_E_RANGE;
+    }
+    if (total == 0) return 0;
+    QkvArgs a{};
+    const int rc = fill_qkv(a, *m, *in, q_out);
+    if (rc) return rc;
+    a.wave_heads = wave_heads_for(*m, total);
+    AttnDesc d{};
+    fill_addressing(d, *m);
+    d.batch = batch;
+    d.ctx_lens = ctx_lens;
+    const int T = g_pools[m->pool].T;
+    PlanBuilder plan(batch);                     // units as in kv_append_chunk
+    for (int s = 0; s < batch; ++s) {
+        if (plan.full()) {
+            HIP_TRY(pkv_launch_qkv_append_chunk(d, a, plan.take(s), g_stream));
+        }
+        plan.add((uint32_t)q_lens[s], q_lens[s] > 0 ? (uint32_t)((q_lens[s] + T - 1) / T + 1) : 0u, 0u, 0u);
+    }
+    HIP_TRY(pkv_launch_qkv_append_chunk(d, a, plan.take(batch), g_stream));
+    return (int)total;
+}
 
 int model_set_batch(int model, int batch, int row_stride) {
     Model *m = get_model(model);

@@ -83,6 +83,19 @@ struct PlanLanes {
         return v;
     }
     __device__ __forceinline__ uint32_t units(const PlanOf<SEQS> &plan) const { return pick(unit, plan.n_seqs); }
+    // which sequence the packed row r belongs to (counted from plan.seq0), and that sequence's first packed row and rows
+    __device__ __forceinline__ PlanUnit find_row(const PlanOf<SEQS> &plan, uint32_t r) const {
+        const int n = plan.n_seqs;
+        int at = -1;
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) at += __popcll(__ballot((int)(threadIdx.x & 63) + 64 * k < n && (row[k] & PKV_PLAN_ROWS) <= r));
+        PlanUnit u;
+        u.seq = plan.seq0 + at;
+        u.unit = u.parts = 0;
+        u.row = (int)(pick(row, at) & PKV_PLAN_ROWS);
+        u.rows = (int)(pick(row, at + 1) & PKV_PLAN_ROWS) - u.row;
+        return u;
+    }
     __device__ __forceinline__ PlanUnit find(const PlanOf<SEQS> &plan, uint32_t u) const {
         const int n = plan.n_seqs;
         int at = -1;

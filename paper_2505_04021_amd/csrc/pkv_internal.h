@@ -148,6 +148,29 @@ inline PlanOf<PKV_PLAN_FEW> few_of(const ChunkPlan &plan) {
     return few;
 }
 
+// What qkv_append[_chunk] does to the rows of a projection before they go on: norms of queries and keys, rotation.
+struct QkvArgs {
+    const uint16_t *q, *k, *v;          // bf16, one token's heads side by side
+    int64_t q_stride, k_stride, v_stride;   // elements from token to token
+    uint16_t *q_out;                    // bf16 [tokens][Hq][D]
+    const uint16_t *q_weight, *k_weight;    // bf16 [D]; NULL: no norm
+    const uint64_t *turns;              // a token's turn of every pair in 2^-64 of a circle; NULL: no rotation
+    const int32_t *before;              // [batch]: tokens in front of a row's first; NULL: none
+    float eps, magnitude;               // magnitude: factor of the rotated elements
+    int32_t rot, pairs;                 // rotated elements; pairs: neighbours are a pair, else e and e + rot / 2
+    int32_t q_aligned;                  // q may be read in 16-byte pieces
+    int32_t wave_heads;                 // query heads of a token that a wave takes
+};
+#define PKV_MAX_ROTARY 64
+
+// The ranges of a launch of kv_gather: rows and units (pages touched) of list entry i, its sequence and first token.
+struct GatherPlan {
+    PlanOf<PKV_PLAN_FEW> rows;
+    struct {
+        int32_t seq, begin;
+    } at[PKV_PLAN_FEW];
+};
+
 #define PKV_MAX_GROUP 16
 #define PKV_PREFILL_WAVES 4     // waves of a prefill work-group
 #define PKV_PREFILL_COLS 128    // MFMA columns (query tokens x heads of the kv head) of a prefill work-group, 32 per wave
@@ -187,10 +210,14 @@ hipError_t pkv_launch_kv_write(const AttnDesc &d, int seq, int tok_begin, int n_
                                const float *ks, const float *vs, int page_tokens, hipStream_t s);
 hipError_t pkv_launch_kv_read(const AttnDesc &d, int seq, int tok_begin, int n_tok, void *k, void *v, float *ks, float *vs,
                               hipStream_t s);
+hipError_t pkv_launch_kv_gather(const AttnDesc &d, const GatherPlan &plan, void *k_out, void *v_out, hipStream_t s);
 // d.batch sequences, d.ctx_lens / d.row_len / d.table as for attention
 hipError_t pkv_launch_kv_append(const AttnDesc &d, const void *k_new, const void *v_new, hipStream_t s);
 // plan: per sequence one unit for every page its new tokens may touch
 hipError_t pkv_launch_kv_append_chunk(const AttnDesc &d, const ChunkPlan &plan, const void *k_new, const void *v_new, hipStream_t s);
+// the same with rows that are normed and rotated first, and the queries of the same tokens: n_rows rows in all
+hipError_t pkv_launch_qkv_append(const AttnDesc &d, const QkvArgs &a, hipStream_t s);
+hipError_t pkv_launch_qkv_append_chunk(const AttnDesc &d, const QkvArgs &a, const ChunkPlan &plan, hipStream_t s);
 // ev: NULL or two events recorded before and after the attention kernel
 enum class AttnForm { ordinary, deep, small };
 hipError_t pkv_launch_attention(const AttnGroup &grp, AttnForm form, hipStream_t s, hipEvent_t *ev);
