@@ -376,6 +376,33 @@ int decode_attention_multi(int n_models, const int *models, const int *batches,
 int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens,
                       const int32_t *ctx_lens, float *out);
 
+/* ---- attention behind shared prefixes ----------------------------------------
+ * Sequences that begin alike (a system prompt, a document, the part that a fork has in common) share the
+ * blocks of those tokens: the prefix lives in a row of its own (any row of the model, filled like any
+ * other, and released when the last sequence has gone; it may also be one of the batch's rows), and a
+ * sequence's row holds what comes behind it.  Whole blocks are shared: the context of sequence s < batch is
+ * the first prefix_blocks[s] blocks of row prefix_seqs[s], all 16 tokens of each, then the ctx_lens[s]
+ * tokens of its own row.  prefix_seqs[s] = -1 or prefix_blocks[s] = 0: no prefix.  Tokens of a prefix
+ * behind its last whole block go into every row that shares it (kv_gather, kv_append_chunk).
+ *   prefix_seqs, prefix_blocks   HOST int32 [batch], read before the call returns
+ * Everything else is as in decode_attention_ex (with the library's table) and prefill_attention: outputs dev
+ * fp32, fp32 accumulation, 16 significant bits of every probability on both cache types, zero rows where nothing is
+ * seen.  PKV_E_RANGE where a row is known to hold fewer blocks than are to be shared; where that turns
+ * out on the device (bookkeeping enqueued and refused), bit 0 of pkv_device_errors() is raised and the rows
+ * of those sequences are zero.  Sums travel through a buffer of the model, made or enlarged when first
+ * needed (PKV_E_NOMEM while the stream is being captured: make the call once before the capture); two calls
+ * of this section on one model must not overlap in time.  Otherwise they only enqueue.
+ *
+ * decode_attention_prefix: q dev bf16 [batch][q_heads][head_dim], out [batch][q_heads][head_dim].  Sequences
+ * with the same prefix_seqs and prefix_blocks form a group; a group's prefix is read once for all its members,
+ * in any order of the batch.
+ * prefill_attention_prefix: query i of sequence s stands behind the prefix and ctx_lens[s] - q_lens[s] + i
+ * tokens of its own and sees all of those and itself. */
+int decode_attention_prefix(int model, int batch, const void *q, const int32_t *prefix_seqs,
+                            const int32_t *prefix_blocks, const int32_t *ctx_lens, float *out);
+int prefill_attention_prefix(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *prefix_seqs,
+                             const int32_t *prefix_blocks, const int32_t *ctx_lens, float *out);
+
 /* ---- observation ----------------------------------------------------------- */
 
 /* Canonical image of the bookkeeping state as little-endian int32 words:

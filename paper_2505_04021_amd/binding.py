@@ -79,6 +79,8 @@ def _load():
         "kv_append": (i, [i, i, vp, vp, vp]),
         "kv_append_chunk": (i, [i, i, vp, vp, vp, vp]),
         "kv_read": (i, [i, i, i, i, vp, vp, vp, vp]),
+        "decode_attention_prefix": (i, [i, i, vp, vp, vp, vp, vp]),
+        "prefill_attention_prefix": (i, [i, i, vp, vp, vp, vp, vp, vp]),
         "kv_gather": (i, [i, i, vp, vp, vp, vp, vp]),
         "rotary_frequencies": (i, [i, C.c_double, i, C.c_double, C.c_double, C.c_double, C.c_double, vp]),
         "rotary_create": (i, [i, i, vp, C.c_double]),
@@ -115,7 +117,7 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
            "pkv_ticket_result", "model_block_table", "kv_write", "kv_append", "kv_append_chunk", "kv_read", "model_set_batch", "decode_attention",
            "decode_attention_ex", "decode_attention_static", "decode_attention_multi", "prefill_attention", "pool_export_state", "pool_stats",
            "arbitrate_requests", "place_models", "rotary_frequencies", "rotary_create", "rotary_destroy", "qkv_append", "qkv_append_chunk",
-           "kv_gather"]
+           "kv_gather", "decode_attention_prefix", "prefill_attention_prefix"]
 
 
 def _f64(a):
@@ -486,6 +488,20 @@ class PrismKV:
         q_lens = np.ascontiguousarray(q_lens, dtype=np.int32)
         return self.lib.prefill_attention(model, q_lens.size, self._p(q), q_lens.ctypes.data_as(C.c_void_p),
                                           self._p(ctx_lens), self._p(out))
+
+    def decode_attention_prefix_dev(self, model, q, prefix_seqs, prefix_blocks, ctx_lens, out):
+        """q, ctx_lens, out: device tensors; prefix_seqs, prefix_blocks: lists or host int32 arrays, one entry a sequence.  Only enqueues."""
+        ps, pb = np.ascontiguousarray(prefix_seqs, dtype=np.int32), np.ascontiguousarray(prefix_blocks, dtype=np.int32)
+        assert ps.size == pb.size == ctx_lens.numel()
+        return self.lib.decode_attention_prefix(model, ps.size, self._p(q), ps.ctypes.data_as(C.c_void_p), pb.ctypes.data_as(C.c_void_p),
+                                                self._p(ctx_lens), self._p(out))
+
+    def prefill_attention_prefix_dev(self, model, q, q_lens, prefix_seqs, prefix_blocks, ctx_lens, out):
+        """The same for packed chunks; q_lens: host int32 array too.  Only enqueues."""
+        ql, ps, pb = (np.ascontiguousarray(x, dtype=np.int32) for x in (q_lens, prefix_seqs, prefix_blocks))
+        assert ql.size == ps.size == pb.size == ctx_lens.numel()
+        return self.lib.prefill_attention_prefix(model, ql.size, self._p(q), ql.ctypes.data_as(C.c_void_p), ps.ctypes.data_as(C.c_void_p),
+                                                 pb.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(out))
 
     def prefill_attention(self, model, q, q_lens, ctx_lens):
         """Convenience for tests: -> (code, out as numpy fp32 [sum q_lens][Hq][D])."""

@@ -65,6 +65,8 @@ struct Elastic {
     int64_t mapped_free = 0;                // of those, frames no model owns
 };
 
+constexpr int kMaxPrefixBuffers = 40;
+
 struct Model {
     bool live = false;
     int pool = -1;
@@ -89,6 +91,11 @@ struct Model {
     size_t cnt_cap = 0;
     float *pf_ws = nullptr;                 // device: partial results of prefill groups whose context is split
     size_t pf_ws_floats = 0;
+    // device: sums of the calls behind shared prefixes.  A buffer that has become too small is kept until the model goes: a captured
+    // graph may still write to it.  (Each is at least twice as large as the one before.)
+    float *px_ws[kMaxPrefixBuffers] = {};
+    int px_buffers = 0;
+    size_t px_ws_floats = 0;                // of the last one
 };
 
 // Uncached device memory for split-K partials and arrival counters.  Blocks are
@@ -272,6 +279,9 @@ void free_model_dev(Model &m) {
     (void)hipFree(m.pf_ws);
     m.pf_ws = nullptr;
     m.pf_ws_floats = 0;
+    for (int i = 0; i < m.px_buffers; ++i) (void)hipFree(m.px_ws[i]);
+    m.px_buffers = 0;
+    m.px_ws_floats = 0;
     m.dev = ModelDev{};
     m.ws = nullptr;
     m.cnt = nullptr;
@@ -461,6 +471,30 @@ int ensure_workspace(Model &m, size_t need_floats, size_t n_cnt, size_t slack = 
         HIP_TRY(hipMemset(m.cnt, 0, n_cnt * slack * sizeof(uint32_t)));
         m.cnt_cap = n_cnt * slack;
     }
+    return PKV_OK;
+}
+
+// The buffer of a model's sums behind shared prefixes, of `need` floats at least.  Made and enlarged without waiting for anything, but not
+// while the stream is being captured.
+int ensure_prefix_ws(Model &m, size_t need, float **ws) {
+    if (need > m.px_ws_floats) {
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        HIP_TRY(hipStreamIsCapturing(g_stream, &capture));
+        if (capture != hipStreamCaptureStatusNone || m.px_buffers == kMaxPrefixBuffers) {
+            snprintf(g_errbuf, sizeof g_errbuf, "a workspace of %zu bytes is needed: make the call once outside of the capture first", need * sizeof(float));
+            return PKV_E_NOMEM;
+        }
+        const size_t floats = need > 2 * m.px_ws_floats ? need : 2 * m.px_ws_floats;
+        float *p = nullptr;
+        if (hipMalloc((void **)&p, floats * sizeof(float)) != hipSuccess) {
+            (void)hipGetLastError();
+            snprintf(g_errbuf, sizeof g_errbuf, "no memory for a workspace of %zu bytes", floats * sizeof(float));
+            return PKV_E_NOMEM;
+        }
+        m.px_ws[m.px_buffers++] = p;
+        m.px_ws_floats = floats;
+    }
+    *ws = m.px_buffers ? m.px_ws[m.px_buffers - 1] : nullptr;
     return PKV_OK;
 }
 
@@ -1989,9 +2023,9 @@ constexpr int kMinPartPairs = 8;        // no part shorter than this
 constexpr double kFillGroups = 1024.0;  // work-groups from which on nothing is cut
 
 // Parts a sequence's groups are cut into when a part should hold about part_pairs page pairs (0: never cut).
-static int prefill_parts(const Model &m, int seq, double part_pairs) {
+static int prefill_parts(int pages, double part_pairs) {
     if (part_pairs <= 0.0) return 1;
-    const int pairs = (m.row_len[seq] + 1) / 2;
+    const int pairs = (pages + 1) / 2;
     int n = (int)(pairs / part_pairs + 0.5);
     if (n > pairs / kMinPartPairs) n = pairs / kMinPartPairs;
     if (n > PKV_PLAN_MAX_PARTS) n = PKV_PLAN_MAX_PARTS;
@@ -2006,7 +2040,10 @@ static int prefill_parts(const Model &m, int seq, double part_pairs) {
 // pairs besides its own.  The parts' partial sums are written and read once, at about 3.5 TB/s.  Cutting up to 1024
 // work-groups whatever that costs, as before, took 135 us for 4 x (2048 + 512) tokens (112 uncut), 55 for 4 x (32 + 512)
 // (29 uncut), 103 for 8 x (4032 + 64) (65 with the cuts chosen here).
-static double prefill_part_pairs(const Model &m, int seq0, int seq1, const int32_t *q_lens, int group) {
+// pages_of(seq): pages of a sequence's context.
+extern "C++" {
+template <typename PAGES>
+static double prefill_part_pairs(const Model &m, int seq0, int seq1, const int32_t *q_lens, int group, const PAGES &pages_of) {
     const double t1 = m.D == 128 ? 0.85 : 0.60, t2 = m.D == 128 ? (m.dtype == PKV_BF16 ? 0.70 : 0.58) : 0.40;
     constexpr double kGroupPairs = 4.0, kCUs = 256.0, kMergeUs = 5.0, kPartBytesPerUs = 3.5e6;
     int longest = 0;
@@ -2014,7 +2051,7 @@ static double prefill_part_pairs(const Model &m, int seq0, int seq1, const int32
     for (int s = seq0; s < seq1; ++s)
         if (q_lens[s] > 0) {
             plain += (q_lens[s] + group - 1) / group;
-            longest = longest > m.row_len[s] ? longest : m.row_len[s];
+            longest = longest > pages_of(s) ? longest : pages_of(s);
         }
     longest = (longest + 1) / 2;
     if (plain * m.Hkv >= kFillGroups || longest < 2 * kMinPartPairs) return 0.0;
@@ -2026,9 +2063,9 @@ static double prefill_part_pairs(const Model &m, int seq0, int seq1, const int32
         double units = 0.0, work = 0.0, top = 0.0, parts_written = 0.0;
         for (int s = seq0; s < seq1; ++s) {
             if (q_lens[s] == 0) continue;
-            const int n = prefill_parts(m, s, part);
+            const int n = prefill_parts(pages_of(s), part);
             const double u = (double)((q_lens[s] + group - 1) / group) * n * m.Hkv;
-            const double len = (double)((m.row_len[s] + 1) / 2) / n + kGroupPairs;
+            const double len = (double)((pages_of(s) + 1) / 2) / n + kGroupPairs;
             units += u;
             work += u * len;
             top = top > len ? top : len;
@@ -2044,8 +2081,23 @@ static double prefill_part_pairs(const Model &m, int seq0, int seq1, const int32
     }
     return best;
 }
+}  // extern "C++"
 
-int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, float *out) {
+// What calls behind shared prefixes are given of them: per sequence the row that holds its prefix and how many of its blocks that is.
+static int check_prefixes(const Model &m, int batch, const int32_t *prefix_seqs, const int32_t *prefix_blocks) {
+    if (!prefix_seqs || !prefix_blocks) return PKV_E_ARG;
+    for (int s = 0; s < batch; ++s) {
+        if (prefix_seqs[s] < -1 || prefix_seqs[s] >= m.dev.max_seqs || prefix_blocks[s] < 0) return PKV_E_ARG;
+        if (prefix_seqs[s] < 0) continue;
+        // (after enqueue-only calls row lengths are estimates; the kernels look at the true ones)
+        if (prefix_blocks[s] > m.dev.max_blocks || (!m.stale && prefix_blocks[s] > m.row_len[prefix_seqs[s]])) return PKV_E_RANGE;
+    }
+    return PKV_OK;
+}
+
+// prefill_attention, and with prefix_seqs prefill_attention_prefix.
+static int run_prefill(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *prefix_seqs, const int32_t *prefix_blocks,
+                       bool prefixed, const int32_t *ctx_lens, float *out) {
     Model *m = get_model(model);
     if (!m) return PKV_E_HANDLE;
     if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
@@ -2062,6 +2114,10 @@ int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens
         total += q_lens[s];
         if (total > (int64_t)1 << 24) return PKV_E_RANGE;
     }
+    if (prefixed) {
+        const int rc = check_prefixes(*m, batch, prefix_seqs, prefix_blocks);
+        if (rc) return rc;
+    }
     if (total == 0) return PKV_OK;
     AttnDesc d{};
     fill_addressing(d, *m);
@@ -2072,41 +2128,167 @@ int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens
     d.cols = tile * m->g;
     d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m->D));
     int split_groups = 0, longest_walk = 0;                // of the launch being put together; pairs of a work-group
+    SharedRows shared;
     auto launch = [&](const ChunkPlan &plan) -> int {
         if (split_groups > 0) {
             const size_t need = (size_t)plan.s[plan.n_seqs].unit * m->Hkv * PKV_PREFILL_COLS * (size_t)(m->D + 4);
-            if (need > m->pf_ws_floats) {
-                HIP_TRY(hipStreamSynchronize(g_stream));
-                (void)hipFree(m->pf_ws);
-                m->pf_ws = nullptr;
-                m->pf_ws_floats = 0;
-                HIP_TRY(hipMalloc((void **)&m->pf_ws, need * sizeof(float)));
-                m->pf_ws_floats = need;
+            if (prefixed) {
+                const int rc = ensure_prefix_ws(*m, need, &d.ws);
+                if (rc) return rc;
+            } else {
+                if (need > m->pf_ws_floats) {
+                    HIP_TRY(hipStreamSynchronize(g_stream));
+                    (void)hipFree(m->pf_ws);
+                    m->pf_ws = nullptr;
+                    m->pf_ws_floats = 0;
+                    HIP_TRY(hipMalloc((void **)&m->pf_ws, need * sizeof(float)));
+                    m->pf_ws_floats = need;
+                }
+                d.ws = m->pf_ws;
             }
-            d.ws = m->pf_ws;
         }
-        HIP_TRY(pkv_launch_prefill(d, plan, split_groups, longest_walk, g_stream));
+        if (prefixed) {
+            HIP_TRY(pkv_launch_prefill_prefixed(d, plan, shared, split_groups, g_stream));
+        } else {
+            HIP_TRY(pkv_launch_prefill(d, plan, split_groups, longest_walk, g_stream));
+        }
         split_groups = longest_walk = 0;
         return PKV_OK;
     };
-    PlanBuilder plan(batch);
+    auto shared_blocks = [&](int s) { return prefixed && prefix_seqs[s] >= 0 ? prefix_blocks[s] : 0; };
+    auto pages_of = [&](int s) { return m->row_len[s] + shared_blocks(s); };
+    PlanBuilder plan(batch, prefixed ? PKV_PLAN_FEW : PKV_PLAN_SEQS);
     double part_pairs = 0.0;
-    g_last_prefill_parts = 1;
+    int most_parts = 1;
     for (int s = 0; s < batch; ++s) {
         if (plan.full()) {
             const int rc = launch(plan.take(s));
             if (rc) return rc;
         }
         if (s % plan.per_launch == 0)
-            part_pairs = prefill_part_pairs(*m, s, s + plan.per_launch < batch ? s + plan.per_launch : batch, q_lens, group);
-        const int parts = prefill_parts(*m, s, part_pairs), groups = (q_lens[s] + group - 1) / group;
-        plan.add((uint32_t)q_lens[s], (uint32_t)(groups * parts), (uint32_t)parts, (uint32_t)(m->row_len[s] / parts));
+            part_pairs = prefill_part_pairs(*m, s, s + plan.per_launch < batch ? s + plan.per_launch : batch, q_lens, group, pages_of);
+        const int parts = prefill_parts(pages_of(s), part_pairs), groups = (q_lens[s] + group - 1) / group;
+        if (prefixed) shared.of[plan.p.n_seqs] = SharedRow{shared_blocks(s) > 0 ? prefix_seqs[s] : 0, shared_blocks(s)};
+        plan.add((uint32_t)q_lens[s], (uint32_t)(groups * parts), (uint32_t)parts, (uint32_t)(pages_of(s) / parts));
         if (parts > 1 && groups > split_groups) split_groups = groups;
-        const int walk = ((m->row_len[s] + 1) / 2 + parts - 1) / parts;
+        const int walk = ((pages_of(s) + 1) / 2 + parts - 1) / parts;
         if (q_lens[s] > 0 && walk > longest_walk) longest_walk = walk;
-        if (q_lens[s] > 0 && parts > g_last_prefill_parts) g_last_prefill_parts = parts;
+        if (q_lens[s] > 0 && parts > most_parts) most_parts = parts;
     }
+    g_last_prefill_parts = most_parts;
     return launch(plan.take(batch));
+}
+
+int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, float *out) {
+    return run_prefill(model, batch, q, q_lens, nullptr, nullptr, false, ctx_lens, out);
+}
+
+int prefill_attention_prefix(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *prefix_seqs, const int32_t *prefix_blocks,
+                             const int32_t *ctx_lens, float *out) {
+    return run_prefill(model, batch, q, q_lens, prefix_seqs, prefix_blocks, true, ctx_lens, out);
+}
+
+// The sequences of a decode_attention_prefix call in the order of their prefixes: (row + 1, blocks, sequence); those without one first.
+static uint64_t g_prefix_order[PKV_MAX_SEQS];
+constexpr double kPrefixUnits = 512.0;        // work-groups that the prefixes of a call are cut into, where they are long enough
+constexpr int kMinPrefixPairs = 8;            // page pairs of such a work-group at least
+
+// The plan of the members from position `at` of the order on; returns the position behind its last one.
+static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, int tile_tok, double part_pairs, uint32_t *tiles_used) {
+    const int size = PKV_PREFILL_WAVES * tile_tok;
+    p.n_groups = p.n_members = 0;
+    uint32_t unit = 0, tile = 0;
+    while (at < batch && p.n_members < PKV_PREFIX_MEMBERS && p.n_groups < PKV_PREFIX_GROUPS) {
+        const uint64_t key = g_prefix_order[at] >> 16;
+        auto &g = p.g[p.n_groups++];
+        const int first = p.n_members;
+        for (; at < batch && p.n_members < PKV_PREFIX_MEMBERS && g_prefix_order[at] >> 16 == key; ++at)
+            p.member[p.n_members++] = (uint16_t)(g_prefix_order[at] & 0xffff);
+        const int blocks = (int)(key & 0xffffff), row = (int)(key >> 24), count = p.n_members - first;
+        const int pairs = (blocks + 1) / 2, wide = (count + size - 1) / size, tiles = (count < size ? count + tile_tok - 1 : size) / tile_tok;
+        int parts = blocks > 0 ? (int)((pairs + part_pairs - 1.0) / part_pairs) : 0;
+        parts = parts > PKV_PLAN_MAX_PARTS ? PKV_PLAN_MAX_PARTS : parts;
+        g.unit = unit;
+        g.first = (uint32_t)first | (uint32_t)(row > 0 ? row - 1 : 0) << 16;
+        g.blocks = (uint32_t)blocks;
+        g.parts = (uint32_t)parts;
+        g.tile = tile;
+        unit += (uint32_t)(wide * parts);
+        tile += (uint32_t)(wide * parts * m.Hkv * tiles);
+    }
+    p.g[p.n_groups].unit = unit;
+    p.g[p.n_groups].first = (uint32_t)p.n_members;
+    p.g[p.n_groups].blocks = p.g[p.n_groups].parts = 0;
+    p.g[p.n_groups].tile = tile;
+    p.prefix_wgs = unit * (uint32_t)m.Hkv;
+    *tiles_used = tile;
+    return at;
+}
+
+int decode_attention_prefix(int model, int batch, const void *q, const int32_t *prefix_seqs, const int32_t *prefix_blocks, const int32_t *ctx_lens,
+                            float *out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0) return PKV_E_ARG;
+    if (batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return PKV_OK;
+    if (!q || !ctx_lens || !out) return PKV_E_ARG;
+    if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return PKV_E_ARG;
+    int rc = check_prefixes(*m, batch, prefix_seqs, prefix_blocks);
+    if (rc) return rc;
+    const int tile_tok = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g, size = PKV_PREFILL_WAVES * tile_tok;
+    for (int s = 0; s < batch; ++s) {
+        const bool has = prefix_seqs[s] >= 0 && prefix_blocks[s] > 0;
+        g_prefix_order[s] = (has ? (uint64_t)(prefix_seqs[s] + 1) << 40 | (uint64_t)prefix_blocks[s] << 16 : 0) | (uint64_t)s;
+    }
+    std::sort(g_prefix_order, g_prefix_order + batch);
+    // how the prefixes are cut
+    double work = 0.0;
+    for (int i = 0, j; i < batch; i = j) {
+        for (j = i + 1; j < batch && g_prefix_order[j] >> 16 == g_prefix_order[i] >> 16;) ++j;
+        const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff);
+        work += (double)((j - i + size - 1) / size) * m->Hkv * ((blocks + 1) / 2);
+    }
+    double part_pairs = work / kPrefixUnits;
+    part_pairs = part_pairs < kMinPrefixPairs ? kMinPrefixPairs : part_pairs;
+    // how the sequences' own rows are
+    int longest = 0;
+    double pages = 0.0;
+    for (int s = 0; s < batch; ++s) {
+        longest = longest > m->row_len[s] ? longest : m->row_len[s];
+        pages += m->row_len[s];
+    }
+    int part = (int)(pages * m->Hkv / kSmallWorkGroups / 8.0 + 1.0) * 8;
+    part = part < kSmallPart[0] ? kSmallPart[0] : part;
+    if ((longest + part - 1) / part > kSmallMaxParts) part = ((longest + kSmallMaxParts - 1) / kSmallMaxParts + 7) / 8 * 8;
+    AttnDesc d{};
+    fill_addressing(d, *m);
+    d.q = (const uint16_t *)q;
+    d.ctx_lens = ctx_lens;
+    d.out = out;
+    d.batch = batch;
+    d.cols = tile_tok * m->g;
+    d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m->D));
+    d.part_pages = part;
+    d.parts = longest > part ? (longest + part - 1) / part : 1;
+    PrefixPlan plan;
+    uint32_t tiles = 0, most = 0;
+    for (int at = 0; at < batch;) {
+        at = take_prefix_plan(plan, *m, batch, at, tile_tok, part_pairs, &tiles);
+        most = most > tiles ? most : tiles;
+    }
+    // (launches come one after the other: the sums of the next plan's prefixes take the place of those that have been joined)
+    const size_t prefix_floats = (size_t)most * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES) * (size_t)(m->D + 4);
+    const size_t own_wgs = (size_t)batch * m->Hkv * d.parts;
+    rc = ensure_prefix_ws(*m, prefix_floats + own_wgs * partial_floats(m->g, m->D), &d.ws);
+    if (rc) return rc;
+    for (int at = 0, n = 0; at < batch; ++n) {
+        at = take_prefix_plan(plan, *m, batch, at, tile_tok, part_pairs, &tiles);
+        plan.own_ws = d.ws + prefix_floats;
+        HIP_TRY(pkv_launch_prefix_sums(d, plan, n == 0 ? (unsigned)own_wgs : 0u, g_stream));
+        HIP_TRY(pkv_launch_prefix_join(d, plan, g_stream));
+    }
+    return PKV_OK;
 }
 
 int decode_attention(int model, const void *q, const int32_t *block_table, const int32_t *ctx_lens, float *out) {

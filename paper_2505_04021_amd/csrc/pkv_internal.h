@@ -171,6 +171,31 @@ struct GatherPlan {
     } at[PKV_PLAN_FEW];
 };
 
+// The row that holds a sequence's shared prefix, and how many of its blocks that is (0: none).
+struct SharedRow {
+    int32_t row, blocks;
+};
+struct SharedRows {
+    SharedRow of[PKV_PLAN_FEW];              // by sequence of the launch
+};
+
+// A launch of decode_attention_prefix: members (sequences) in the order of their groups; a group's members share a prefix.
+#define PKV_PREFIX_GROUPS 64
+#define PKV_PREFIX_MEMBERS 512
+struct PrefixPlan {
+    int32_t n_groups, n_members;
+    uint32_t prefix_wgs;                     // work-groups for the prefixes, the launch's first
+    float *own_ws;                           // sums of the parts of the sequences' own rows (d.ws: those of the prefixes)
+    struct {
+        uint32_t unit;                       // its first unit
+        uint32_t first;                      // its first member | row of the prefix << 16
+        uint32_t blocks;
+        uint32_t parts;                      // of the prefix
+        uint32_t tile;                       // its first tile of 32 columns of d.ws
+    } g[PKV_PREFIX_GROUPS + 1];              // [n_groups]: units and members in total
+    uint16_t member[PKV_PREFIX_MEMBERS];
+};
+
 #define PKV_MAX_GROUP 16
 #define PKV_PREFILL_WAVES 4     // waves of a prefill work-group
 #define PKV_PREFILL_COLS 128    // MFMA columns (query tokens x heads of the kv head) of a prefill work-group, 32 per wave
@@ -229,3 +254,8 @@ hipError_t pkv_launch_attention_static(const AttnGroup &grp, uint32_t *cnt, size
 // longest_walk: page pairs that a unit walks at most, as far as the host knows
 hipError_t pkv_launch_prefill(const AttnDesc &d, const ChunkPlan &plan, int split_groups, int longest_walk, hipStream_t s);
 hipError_t pkv_launch_stream_read(const void *src, size_t bytes, size_t granule_bytes, uint32_t *sink, hipStream_t s);
+// the same with contexts that begin with blocks of other rows; at most PKV_PLAN_FEW sequences
+hipError_t pkv_launch_prefill_prefixed(const AttnDesc &d, const ChunkPlan &plan, const SharedRows &shared, int split_groups, hipStream_t s);
+// decode behind shared prefixes: sums of the prefixes and (own_wgs > 0) of all d.batch sequences' own rows; then the rows of a plan's members
+hipError_t pkv_launch_prefix_sums(const AttnDesc &d, const PrefixPlan &plan, unsigned own_wgs, hipStream_t s);
+hipError_t pkv_launch_prefix_join(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);

@@ -51,22 +51,28 @@ def turned(x, pos, weight=None, eps=1e-6, rot=0, pairs=False, freq=None, magnitu
 
 
 def attention(q, k, v, limits):
-    """softmax(q K^T / sqrt(D)) V: q [n][Hq][D], k and v [tokens][Hkv][D] float64; row i sees the first limits[i] tokens, none: zeros."""
+    """softmax(q K^T / sqrt(D)) V: q [n][Hq][D], k and v [tokens][Hkv][D] float64; row i sees the first limits[i] tokens, none: zeros.
+    Also how far fp32 sums with probabilities of 16 significant bits may be off, element by element: relative to sum_t p_t |v_t|,
+    2^-17 for the rounding of p with as much again for exponentials, sums and products, and what a logit is off by, which is some steps
+    of 2^-24 of sum |q k| / sqrt(D): 2^-19 of it."""
     n, hq, d = q.shape
-    hkv = k.shape[1]
-    out = np.zeros((n, hq, d))
-    for i in range(n):
-        m = limits[i]
-        if m <= 0:
-            continue
-        for h in range(hkv):
-            qs = q[i, h * (hq // hkv):(h + 1) * (hq // hkv)]
-            z = qs @ k[:m, h].T / np.sqrt(d)
-            top = z.max(axis=-1, keepdims=True)
-            p = np.exp(z - np.where(np.isfinite(top), top, 0.0))
-            den = p.sum(axis=-1, keepdims=True)
-            out[i, h * (hq // hkv):(h + 1) * (hq // hkv)] = np.divide(p @ v[:m, h], den, out=np.zeros_like(qs), where=den > 0)
-    return out
+    hkv, g = k.shape[1], q.shape[1] // k.shape[1]
+    out, tol = np.zeros((n, hq, d)), np.zeros((n, hq, d))
+    top = max(limits, default=0)
+    if top <= 0:
+        return out, tol
+    seen = np.arange(top)[None, :] < np.asarray(limits)[:, None]
+    for h in range(hkv):
+        for j in range(h * g, (h + 1) * g):
+            z = np.where(seen, q[:, j] @ k[:top, h].T / np.sqrt(d), -np.inf)
+            far = np.where(seen, np.abs(q[:, j]) @ np.abs(k[:top, h]).T / np.sqrt(d), 0.0).max(axis=1, keepdims=True)
+            m = z.max(axis=1, keepdims=True)
+            p = np.exp(z - np.where(np.isfinite(m), m, 0.0))
+            den = p.sum(axis=1, keepdims=True)
+            p = np.divide(p, den, out=np.zeros_like(p), where=den > 0)
+            out[:, j] = p @ v[:top, h]
+            tol[:, j] = (2.0 ** -16 + 2.0 ** -19 * far) * (p @ np.abs(v[:top, h]))
+    return out, tol
 
 
 class Cache:
