@@ -2190,11 +2190,22 @@ int prefill_attention_prefix(int model, int batch, const void *q, const int32_t 
 
 // The sequences of a decode_attention_prefix call in the order of their prefixes: (row + 1, blocks, sequence); those without one first.
 static uint64_t g_prefix_order[PKV_MAX_SEQS];
-constexpr double kPrefixUnits = 512.0;        // work-groups that the prefixes of a call are cut into, where they are long enough
-constexpr int kMinPrefixPairs = 8;            // page pairs of such a work-group at least
+
+// How the call is cut: page pairs of a part of a prefix, pages of a part of an own row.
+struct PrefixCut {
+    double pairs;
+    int pages;
+};
+
+constexpr int kMinPrefixPairs = 4;            // page pairs of a part of a prefix at least
+
+static int prefix_parts(int blocks, double part_pairs) {
+    const int pairs = (blocks + 1) / 2, n = (int)(pairs / part_pairs + 0.999);
+    return blocks == 0 ? 0 : (n < 1 ? 1 : (n > PKV_PLAN_MAX_PARTS ? PKV_PLAN_MAX_PARTS : n));
+}
 
 // The plan of the members from position `at` of the order on; returns the position behind its last one.
-static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, int tile_tok, double part_pairs, uint32_t *tiles_used) {
+static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, int tile_tok, const PrefixCut &cut) {
     const int size = PKV_PREFILL_WAVES * tile_tok;
     p.n_groups = p.n_members = 0;
     uint32_t unit = 0, tile = 0;
@@ -2205,24 +2216,97 @@ static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, in
         for (; at < batch && p.n_members < PKV_PREFIX_MEMBERS && g_prefix_order[at] >> 16 == key; ++at)
             p.member[p.n_members++] = (uint16_t)(g_prefix_order[at] & 0xffff);
         const int blocks = (int)(key & 0xffffff), row = (int)(key >> 24), count = p.n_members - first;
-        const int pairs = (blocks + 1) / 2, wide = (count + size - 1) / size, tiles = (count < size ? count + tile_tok - 1 : size) / tile_tok;
-        int parts = blocks > 0 ? (int)((pairs + part_pairs - 1.0) / part_pairs) : 0;
-        parts = parts > PKV_PLAN_MAX_PARTS ? PKV_PLAN_MAX_PARTS : parts;
+        const int wide = (count + size - 1) / size, tiles = count < size ? (count + tile_tok - 1) / tile_tok : PKV_PREFILL_WAVES;
+        const int parts = prefix_parts(blocks, cut.pairs);
         g.unit = unit;
         g.first = (uint32_t)first | (uint32_t)(row > 0 ? row - 1 : 0) << 16;
-        g.blocks = (uint32_t)blocks;
-        g.parts = (uint32_t)parts;
+        g.blocks = (uint32_t)blocks | (uint32_t)parts << 24;
         g.tile = tile;
         unit += (uint32_t)(wide * parts);
         tile += (uint32_t)(wide * parts * m.Hkv * tiles);
     }
     p.g[p.n_groups].unit = unit;
     p.g[p.n_groups].first = (uint32_t)p.n_members;
-    p.g[p.n_groups].blocks = p.g[p.n_groups].parts = 0;
+    p.g[p.n_groups].blocks = 0;
     p.g[p.n_groups].tile = tile;
     p.prefix_wgs = unit * (uint32_t)m.Hkv;
-    *tiles_used = tile;
+    // the members' own rows, longest first
+    uint64_t by_length[PKV_PREFIX_MEMBERS];
+    for (int i = 0; i < p.n_members; ++i) by_length[i] = (uint64_t)(uint32_t)m.row_len[p.member[i]] << 32 | (uint32_t)(PKV_PREFIX_MEMBERS - i);
+    std::sort(by_length, by_length + p.n_members, std::greater<uint64_t>());
+    int with[PKV_PLAN_MAX_PARTS] = {};                    // rows with a k-th part
+    for (int r = 0; r < p.n_members; ++r) {
+        const int i = PKV_PREFIX_MEMBERS - (int)(uint32_t)by_length[r], pages = (int)(by_length[r] >> 32);
+        p.own[r] = p.member[i];
+        p.rank[i] = (uint16_t)r;
+        int parts = (pages + cut.pages - 1) / cut.pages;
+        parts = parts < 1 ? 1 : (parts > PKV_PLAN_MAX_PARTS ? PKV_PLAN_MAX_PARTS : parts);
+        for (int k = 0; k < parts; ++k) with[k] = r + 1;
+    }
+    p.own_unit[0] = 0;
+    for (int k = 0; k < PKV_PLAN_MAX_PARTS; ++k) p.own_unit[k + 1] = p.own_unit[k] + (uint32_t)with[k];
     return at;
+}
+
+// Parts of own rows: some 768 work-groups in all (us a step, 24, 40, 64 and 256 pages a part: 64 rows around 400 tokens of 32/8/128 47.0, 47.3, 48.8,
+// 49.3 behind a prefix and 34.6, 36.1, 39.4, 42.6 without; 96 around 700 on e4m3 caches 47.5, 46.5, 47.5, 45.5 and 38.5, 37.1, 38.6, 40.4).
+//
+// Parts of prefixes: of some numbers of cuts the one that is estimated to be the cheapest.  A work-group alone on its CU takes t1 us a
+// page pair, two of them together up to 2 t2 (measured: prefixes of 1024 to 8192 tokens in 8 to 640 work-groups).  Own rows are read
+// beside them: they slow the longest walk down, and take their bytes' time and most of what the prefixes' products cost; what the two
+// come to together lies between the larger one and the sum.  Every part's sums are written and read again.  Us a step with 1, 2, 4, 8, 16
+// and 32 cuts: 64 rows of 32/8/128 around 400 tokens behind 4096 97.8, 60.2, 42.2, 45.1, 51.8, 65.1 (without tokens of their own 89.2, 50.4,
+// 31.2, 23.0, 22.4, 29.3); seven tenants on e4m3 caches 86.5, 55.0, 45.6, 49.6, 56.1, 62.0; 96 rows of 64/8/128 behind 24576 tokens with 4, 5, 8, 9,
+// 10 and 11 cuts 143.7, 130.3, 122.6, 117.4, 119.9, 154.8 (with 11 more than 512 work-groups).  On 70 random calls the choice takes 3 to 5 % more than
+// the best of a dozen numbers.
+static PrefixCut cut_prefixes(const Model &m, int batch, int tile_tok) {
+    constexpr double kOwnWorkGroups = 768.0, kCUs = 256.0, kPartBytesPerUs = 3.0e6;
+    const int size = PKV_PREFILL_WAVES * tile_tok;
+    PrefixCut cut;
+    double pages = 0.0;
+    int longest_row = 0, longest = 0;
+    for (int s = 0; s < batch; ++s) {
+        const int blocks = (int)(g_prefix_order[s] >> 16 & 0xffffff);
+        longest = longest > blocks ? longest : blocks;
+        longest_row = longest_row > m.row_len[s] ? longest_row : m.row_len[s];
+        pages += m.row_len[s];
+    }
+    cut.pages = (int)(pages * m.Hkv / kOwnWorkGroups / 8.0 + 1.0) * 8;
+    cut.pages = cut.pages < kSmallPart[0] ? kSmallPart[0] : cut.pages;
+    if (longest_row > cut.pages * PKV_PLAN_MAX_PARTS) cut.pages = (longest_row + PKV_PLAN_MAX_PARTS * 8 - 1) / (PKV_PLAN_MAX_PARTS * 8) * 8;
+    longest = (longest + 1) / 2;
+    cut.pairs = longest > 0 ? longest : 1.0;
+    const double t1 = m.dtype == PKV_BF16 ? (m.D == 128 ? 0.60 : 0.43) : (m.D == 128 ? 0.71 : 0.57), t2 = m.D == 128 ? 1.13 * t1 : 0.95 * t1;
+    const double own_us = pages * (double)m.layer_bytes / 6.0e6;
+    static const int kCuts[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64};
+    double best_us = 1e30;
+    for (int cuts : kCuts) {
+        const double part = (double)longest / cuts;
+        if (cuts > 1 && part < kMinPrefixPairs) break;
+        double units = 0.0, work = 0.0, top = 0.0, tiles = 0.0;
+        for (int i = 0, j; i < batch; i = j) {
+            for (j = i + 1; j < batch && g_prefix_order[j] >> 16 == g_prefix_order[i] >> 16;) ++j;
+            const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff), n = prefix_parts(blocks, part);
+            if (n == 0) continue;
+            const double u = (double)((j - i + size - 1) / size) * n * m.Hkv, len = (double)((blocks + 1) / 2) / n;
+            units += u;
+            work += u * len;
+            top = top > len ? top : len;
+            tiles += (double)((j - i + tile_tok - 1) / tile_tok) * n * m.Hkv;
+        }
+        const double even = work / kCUs * t2, both = units <= kCUs ? 0.0 : (units < 2.0 * kCUs ? units / kCUs - 1.0 : 1.0);
+        const double one = t1 * (1.0 + 0.15 * fmin(units / kCUs, 1.0));                  // (busy CUs slow each other down: power)
+        double walk = top * (one + (2.0 * t2 - one) * both);
+        if (units > 2.0 * kCUs) walk = fmax(even, walk * ceil(units / (2.0 * kCUs)));
+        walk += fmin(own_us * (1.3 - both), 0.35 * walk);
+        const double rest = own_us + 0.7 * even;
+        const double us = cbrt(walk * walk * walk + rest * rest * rest) + tiles * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES * (m.D + 4) * 4 * 2) / kPartBytesPerUs;
+        if (us < best_us) {
+            best_us = us;
+            cut.pairs = part;
+        }
+    }
+    return cut;
 }
 
 int decode_attention_prefix(int model, int batch, const void *q, const int32_t *prefix_seqs, const int32_t *prefix_blocks, const int32_t *ctx_lens,
@@ -2236,31 +2320,13 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
     if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return PKV_E_ARG;
     int rc = check_prefixes(*m, batch, prefix_seqs, prefix_blocks);
     if (rc) return rc;
-    const int tile_tok = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g, size = PKV_PREFILL_WAVES * tile_tok;
     for (int s = 0; s < batch; ++s) {
         const bool has = prefix_seqs[s] >= 0 && prefix_blocks[s] > 0;
         g_prefix_order[s] = (has ? (uint64_t)(prefix_seqs[s] + 1) << 40 | (uint64_t)prefix_blocks[s] << 16 : 0) | (uint64_t)s;
     }
     std::sort(g_prefix_order, g_prefix_order + batch);
-    // how the prefixes are cut
-    double work = 0.0;
-    for (int i = 0, j; i < batch; i = j) {
-        for (j = i + 1; j < batch && g_prefix_order[j] >> 16 == g_prefix_order[i] >> 16;) ++j;
-        const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff);
-        work += (double)((j - i + size - 1) / size) * m->Hkv * ((blocks + 1) / 2);
-    }
-    double part_pairs = work / kPrefixUnits;
-    part_pairs = part_pairs < kMinPrefixPairs ? kMinPrefixPairs : part_pairs;
-    // how the sequences' own rows are
-    int longest = 0;
-    double pages = 0.0;
-    for (int s = 0; s < batch; ++s) {
-        longest = longest > m->row_len[s] ? longest : m->row_len[s];
-        pages += m->row_len[s];
-    }
-    int part = (int)(pages * m->Hkv / kSmallWorkGroups / 8.0 + 1.0) * 8;
-    part = part < kSmallPart[0] ? kSmallPart[0] : part;
-    if ((longest + part - 1) / part > kSmallMaxParts) part = ((longest + kSmallMaxParts - 1) / kSmallMaxParts + 7) / 8 * 8;
+    const int tile_tok = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g;
+    const PrefixCut cut = cut_prefixes(*m, batch, tile_tok);
     AttnDesc d{};
     fill_addressing(d, *m);
     d.q = (const uint16_t *)q;
@@ -2269,24 +2335,30 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
     d.batch = batch;
     d.cols = tile_tok * m->g;
     d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m->D));
-    d.part_pages = part;
-    d.parts = longest > part ? (longest + part - 1) / part : 1;
+    d.part_pages = cut.pages;
+    // Plans come one after the other, sums and join, so that the next one's sums take the place of those that have been joined.
     PrefixPlan plan;
-    uint32_t tiles = 0, most = 0;
-    for (int at = 0; at < batch;) {
-        at = take_prefix_plan(plan, *m, batch, at, tile_tok, part_pairs, &tiles);
-        most = most > tiles ? most : tiles;
+    size_t prefix_floats = 0, own_floats = 0;
+    auto floats = [&](size_t &prefix, size_t &own) {
+        prefix = (size_t)plan.g[plan.n_groups].tile * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES) * (size_t)(m->D + 4);
+        own = (size_t)plan.own_unit[PKV_PLAN_MAX_PARTS] * m->Hkv * partial_floats(m->g, m->D);
+    };
+    int end = take_prefix_plan(plan, *m, batch, 0, tile_tok, cut);
+    floats(prefix_floats, own_floats);
+    for (int at = end; at < batch;) {
+        size_t a, b;
+        at = take_prefix_plan(plan, *m, batch, at, tile_tok, cut);
+        floats(a, b);
+        prefix_floats = prefix_floats > a ? prefix_floats : a;
+        own_floats = own_floats > b ? own_floats : b;
     }
-    // (launches come one after the other: the sums of the next plan's prefixes take the place of those that have been joined)
-    const size_t prefix_floats = (size_t)most * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES) * (size_t)(m->D + 4);
-    const size_t own_wgs = (size_t)batch * m->Hkv * d.parts;
-    rc = ensure_prefix_ws(*m, prefix_floats + own_wgs * partial_floats(m->g, m->D), &d.ws);
+    rc = ensure_prefix_ws(*m, prefix_floats + own_floats, &d.ws);
     if (rc) return rc;
-    for (int at = 0, n = 0; at < batch; ++n) {
-        at = take_prefix_plan(plan, *m, batch, at, tile_tok, part_pairs, &tiles);
+    const bool one = end == batch;
+    for (int at = 0; at < batch;) {
+        at = one ? end : take_prefix_plan(plan, *m, batch, at, tile_tok, cut);
         plan.own_ws = d.ws + prefix_floats;
-        HIP_TRY(pkv_launch_prefix_sums(d, plan, n == 0 ? (unsigned)own_wgs : 0u, g_stream));
-        HIP_TRY(pkv_launch_prefix_join(d, plan, g_stream));
+        HIP_TRY(pkv_launch_prefix(d, plan, g_stream));
     }
     return PKV_OK;
 }

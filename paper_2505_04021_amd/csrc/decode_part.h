@@ -334,9 +334,16 @@ constexpr int SMALL_WAVES = 4;
 // have all waves of a part.
 __device__ __forceinline__ float merge_weight(float m, float M) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M); }
 
-// JOIN: parts are joined here and rows written; otherwise every part leaves its sums (partial_floats) at `sums` for another kernel.
+// A part of a row for a kernel that joins the parts itself: which, of how many, and where its sums (partial_floats) go.
+struct RowPart {
+    int seq, kvh, part, parts;
+    float *sums;
+};
+
+// JOIN: parts are joined here and rows written; wg: the work-group's number among its model's.  Otherwise the part that `at_part` says leaves its
+// sums, also where the row turns out not to have it (then maxima of -inf and denominators of 0, the others as they are).
 template <int D, int DT, bool JOIN = true>
-__device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_acc, float *s_m, float *s_l, uint32_t *s_arrived, float *sums = nullptr) {
+__device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_acc, float *s_m, float *s_l, uint32_t *s_arrived, const RowPart *at_part = nullptr) {
     using TL = Tile<D, DT>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int G = lane >> 4, n = lane & 15, g = d.g;
@@ -345,7 +352,11 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     // with the parts slowest.  Otherwise parts come slowest, so that the first parts, which every row has, fall on all
     // XCDs (100 rows of 2 kv heads, parts before rows: 40 us, twice the ordinary form).
     int seq, kvh, part;
-    if ((d.Hkv & 7) == 0) {
+    if constexpr (!JOIN) {
+        seq = at_part->seq;
+        kvh = at_part->kvh;
+        part = at_part->part;
+    } else if ((d.Hkv & 7) == 0) {
         const int per_row = d.Hkv * d.parts, rest = wg % per_row;
         seq = wg / per_row;
         part = rest / d.Hkv;
@@ -372,15 +383,21 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     const int L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
     const int n_pages = (L + T - 1) / T;
     int size = d.part_pages;
-    if (n_pages > d.parts * size) {                       // longer than the host knew
-        size = (n_pages + d.parts - 1) / d.parts;
+    if (n_pages > (JOIN ? d.parts : at_part->parts) * size) {                       // longer than the host knew
+        size = (n_pages + (JOIN ? d.parts : at_part->parts) - 1) / (JOIN ? d.parts : at_part->parts);
         size = (size + STEP - 1) / STEP * STEP;
         page0 = part * size + 2 * w;
         ids = fetch_ids(d, row, page0);
         id = id_of(page0 + STEP + ahead);
     }
     const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
-    if (part >= n_parts) return;
+    if (part >= n_parts) {
+        if (!JOIN && (int)threadIdx.x < g) {
+            at_part->sums[g * D + threadIdx.x] = -INFINITY;
+            at_part->sums[g * D + g + threadIdx.x] = 0.f;
+        }
+        return;
+    }
     const int pe = (part + 1) * size < n_pages ? (part + 1) * size : n_pages;
     const int last_valid = L - (n_pages - 1) * T;
     State<D, DT> st;
@@ -530,7 +547,7 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     // the sums of the work-group: lane by lane four output elements of one head
     const int quads = g * (D / 4), pf = partial_floats(g, D);
     const bool whole = JOIN && n_parts == 1;
-    float *mine = (JOIN ? d.ws : sums) + (size_t)(seg * d.parts + part) * pf;
+    float *mine = JOIN ? d.ws + (size_t)(seg * d.parts + part) * pf : at_part->sums;
     for (int i = threadIdx.x; i < quads; i += 64 * SMALL_WAVES) {
         const int hn = i / (D / 4), x = i - hn * (D / 4);
         float M = s_m[hn];

@@ -179,21 +179,25 @@ struct SharedRows {
     SharedRow of[PKV_PLAN_FEW];              // by sequence of the launch
 };
 
-// A launch of decode_attention_prefix: members (sequences) in the order of their groups; a group's members share a prefix.
+// A launch of decode_attention_prefix: members (sequences) in the order of their groups; a group's members share a prefix.  Their own rows
+// fall into parts; the first parts of all rows come first, then all second parts and so on, longer rows first, so that the rows that
+// have a k-th part are the first ones of that order and a list of counts is all there is to say.
 #define PKV_PREFIX_GROUPS 64
-#define PKV_PREFIX_MEMBERS 512
+#define PKV_PREFIX_MEMBERS 384
 struct PrefixPlan {
     int32_t n_groups, n_members;
     uint32_t prefix_wgs;                     // work-groups for the prefixes, the launch's first
-    float *own_ws;                           // sums of the parts of the sequences' own rows (d.ws: those of the prefixes)
+    float *own_ws;                           // sums of the own rows' parts, by unit and kv head (d.ws: those of the prefixes)
     struct {
         uint32_t unit;                       // its first unit
         uint32_t first;                      // its first member | row of the prefix << 16
-        uint32_t blocks;
-        uint32_t parts;                      // of the prefix
+        uint32_t blocks;                     // of the prefix | parts that it comes in << 24
         uint32_t tile;                       // its first tile of 32 columns of d.ws
     } g[PKV_PREFIX_GROUPS + 1];              // [n_groups]: units and members in total
-    uint16_t member[PKV_PREFIX_MEMBERS];
+    uint32_t own_unit[PKV_PLAN_MAX_PARTS + 1];   // the first unit of all k-th parts; [64]: units in total, and so where there is no k-th part
+    uint16_t member[PKV_PREFIX_MEMBERS];     // sequences by group
+    uint16_t own[PKV_PREFIX_MEMBERS];        // sequences by length
+    uint16_t rank[PKV_PREFIX_MEMBERS];       // member -> its place by length
 };
 
 #define PKV_MAX_GROUP 16
@@ -256,6 +260,5 @@ hipError_t pkv_launch_prefill(const AttnDesc &d, const ChunkPlan &plan, int spli
 hipError_t pkv_launch_stream_read(const void *src, size_t bytes, size_t granule_bytes, uint32_t *sink, hipStream_t s);
 // the same with contexts that begin with blocks of other rows; at most PKV_PLAN_FEW sequences
 hipError_t pkv_launch_prefill_prefixed(const AttnDesc &d, const ChunkPlan &plan, const SharedRows &shared, int split_groups, hipStream_t s);
-// decode behind shared prefixes: sums of the prefixes and (own_wgs > 0) of all d.batch sequences' own rows; then the rows of a plan's members
-hipError_t pkv_launch_prefix_sums(const AttnDesc &d, const PrefixPlan &plan, unsigned own_wgs, hipStream_t s);
-hipError_t pkv_launch_prefix_join(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);
+// decode behind shared prefixes: the sums of the prefixes and of the members' own rows, then the rows that they join to
+hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);

@@ -51,7 +51,7 @@ __device__ __forceinline__ GroupInfo group_info(const AttnDesc &d, const PlanOf<
 
 // A group of a chunk's query tokens in front of its own row.
 struct ChunkUnit {
-    static constexpr bool CAUSAL = true;
+    static constexpr bool CAUSAL = true, LEVELS = true;
     int seq, q0, ntok, back, part, parts, slot;
     const int32_t *own;
     __device__ __forceinline__ ChunkUnit(const GroupInfo &g, const AttnDesc &d, int group)

@@ -381,7 +381,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     // (The waves meet in every second or fourth step, for the last time in step np - 2 or before.  Rounded to such a step the last one
     // never comes in walks of up to 29 and odd numbers up to 43 pairs (bf16), of up to 17 and half of those up to 57 (e4m3): these end a level
     // or two above 0.  Moved to the last meeting, so that all end on it, launches take as long or up to 1 % longer.)
-    constexpr bool LEVELS = D == 128;
+    constexpr bool LEVELS = D == 128 && UNIT::LEVELS;
     const int first_step = (np / 2 + np / 32 + MEET / 2) & -MEET, second_step = (np - np / 5 + MEET / 2) & -MEET, third_step = (np - np / 15 + MEET / 2) & -MEET;
     if constexpr (LEVELS) __builtin_amdgcn_s_setprio(3);
 

@@ -11,23 +11,38 @@
 
 namespace {
 
-// A group of a plan, found by one read for all lanes.
+// The groups of a plan and the counts of parts, one of each a lane, by one read.
 struct GroupLanes {
-    uint32_t unit, first, blocks, parts, tile;
+    uint32_t unit, first, blocks, tile;
     __device__ __forceinline__ explicit GroupLanes(const PrefixPlan &plan) {
         const int i = threadIdx.x & 63;
         unit = plan.g[i].unit;
         first = plan.g[i].first;
         blocks = plan.g[i].blocks;
-        parts = plan.g[i].parts;
         tile = plan.g[i].tile;
     }
     static __device__ __forceinline__ uint32_t of(uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)x, i); }
+    __device__ __forceinline__ int first_member(const PrefixPlan &plan, int i) const {
+        return (int)((i < 64 ? of(first, i) : plan.g[64].first) & 0xffffu);
+    }
 };
-static_assert(PKV_PREFIX_GROUPS == 64, "a group per lane");
+static_assert(PKV_PREFIX_GROUPS == 64 && PKV_PLAN_MAX_PARTS == 64, "one of each per lane");
+
+// How a group's members fall into work-groups and tiles of 32 columns.
+struct GroupShape {
+    int size, wide, tiles;                // members of a work-group, work-groups side by side, tiles of each
+    __device__ __forceinline__ GroupShape(const AttnDesc &d, int count) {
+        const int tile_tok = d.cols / d.g;
+        size = PF_WAVES * tile_tok;
+        wide = (count + size - 1) / size;
+        tiles = count < size ? (count + tile_tok - 1) / tile_tok : PF_WAVES;
+    }
+};
 
 struct PrefixUnit {
     static constexpr bool CAUSAL = false;
+    // (96 rows behind 24576 tokens, without their own, in 192 work-groups 138, 146 us without levels, in 400 112.5, 115.7)
+    static constexpr bool LEVELS = true;
     const uint16_t *members;
     const int32_t *shared;
     int prefix_row, blocks, ntok, part, parts, tiles, first_tile;      // (tiles: of 32 columns, in the unit)
@@ -37,19 +52,19 @@ struct PrefixUnit {
         const int n = plan.n_groups;
         // groups without units share their first unit with the next one
         const int at = __popcll(__ballot((int)(threadIdx.x & 63) < n && lanes.unit <= (uint32_t)unit)) - 1;
-        const uint32_t f = lanes.of(lanes.first, at);
-        const int first = (int)(f & 0xffffu), end = at + 1 < 64 ? (int)(lanes.of(lanes.first, at + 1) & 0xffffu) : (int)(plan.g[64].first & 0xffffu);
-        const int tile_tok = d.cols / d.g, size = PF_WAVES * tile_tok, count = end - first, wide = (count + size - 1) / size;
+        const uint32_t f = lanes.of(lanes.first, at), b = lanes.of(lanes.blocks, at);
+        const int first = (int)(f & 0xffffu), count = lanes.first_member(plan, at + 1) - first;
+        const GroupShape shape(d, count);
         const int u = unit - (int)lanes.of(lanes.unit, at);
-        part = u / wide;
-        const int x = u - part * wide;
-        members = plan.member + first + x * size;
-        ntok = count - x * size < size ? count - x * size : size;
-        blocks = (int)lanes.of(lanes.blocks, at);
-        parts = (int)lanes.of(lanes.parts, at);
+        part = u / shape.wide;
+        const int x = u - part * shape.wide;
+        members = plan.member + first + x * shape.size;
+        ntok = count - x * shape.size < shape.size ? count - x * shape.size : shape.size;
+        blocks = (int)(b & 0xffffffu);
+        parts = (int)(b >> 24);
         prefix_row = (int)(f >> 16);
         shared = d.table + (size_t)prefix_row * d.row_stride;
-        tiles = (count < size ? count + tile_tok - 1 : size) / tile_tok;
+        tiles = shape.tiles;
         first_tile = (int)lanes.of(lanes.tile, at) + u * d.Hkv * tiles;
     }
     __device__ __forceinline__ uint32_t id(const AttnDesc &d, int page) const { return (uint32_t)shared[page < d.row_stride ? page : d.row_stride - 1]; }
@@ -70,80 +85,101 @@ __global__ __launch_bounds__(64 * PF_WAVES, 2) void k_prefix_sums(const AttnDesc
     constexpr int OWN = SMALL_WAVES * 16 * D * 4 + 2 * SMALL_WAVES * 16 * 4, RING = kRingBytes<D, DT, MEET>;
     __shared__ __align__(16) uint8_t lds[OWN > RING ? OWN : RING];
     static_assert(PF_WAVES == SMALL_WAVES, "one size of work-group");
+    // Prefixes first: their walks are the longest.  (Own rows first: with the best number of cuts for either 64 rows behind 4096 tokens 42.2 and 45.8 us, 96 behind 24576 117.4 and
+    // 124.6, seven tenants on e4m3 caches 45.6 and 47.6.)
     if (blockIdx.x < plan.prefix_wgs) {
         const int unit = blockIdx.x / d.Hkv, kvh = blockIdx.x - unit * d.Hkv;
         prefill_unit<D, DT, MEET, true>(d, PrefixUnit(d, plan, unit), kvh, lds);
     } else {
         float *acc = reinterpret_cast<float *>(lds), *m = acc + SMALL_WAVES * 16 * D, *l = m + SMALL_WAVES * 16;
-        attn_part<D, DT, false>(d, (int)(blockIdx.x - plan.prefix_wgs), acc, m, l, nullptr, plan.own_ws);
+        const int x = (int)(blockIdx.x - plan.prefix_wgs), unit = x / d.Hkv, lane = threadIdx.x & 63;
+        const uint32_t from = plan.own_unit[lane], to = plan.own_unit[lane + 1];
+        RowPart at;
+        at.kvh = x - unit * d.Hkv;
+        at.part = __popcll(__ballot(from <= (uint32_t)unit)) - 1;
+        const int rank = unit - (int)GroupLanes::of(from, at.part);
+        at.parts = __popcll(__ballot(to - from > (uint32_t)rank));
+        at.seq = __builtin_amdgcn_readfirstlane((int)plan.own[rank]);
+        at.sums = plan.own_ws + (size_t)x * partial_floats(d.g, D);
+        attn_part<D, DT, false>(d, 0, acc, m, l, nullptr, &at);
     }
 }
 
-// One wave per (member, query head): lane i holds the maxima and denominators of parts i and i + 64, then D / 4 lanes take the sums of a
-// part, 64 * 4 / D parts side by side.  Bound by memory trips: the plan, the lengths, maxima and denominators, sums.
+// One wave per (member, query head): lane k holds the maximum and denominator of part k of the prefix and of the own row, then D / 4 lanes
+// take the sums of a part, 256 / D parts side by side.  Bound by memory trips, two behind the plan: all of a row's maxima and
+// denominators travel with the first sums.
 constexpr int JOIN_WAVES = 4;
 
 template <int D>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc d, const PrefixPlan plan) {
-    constexpr int QUADS = D / 4, SIDE = 64 / QUADS;
+    constexpr int QUADS = D / 4, SIDE = 64 / QUADS, TRIP = 8;
     const int lane = threadIdx.x & 63;
     const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6)));
     const int j = x / d.Hq, hq = x - j * d.Hq;
     if (j >= plan.n_members) return;
     const GroupLanes lanes(plan);
+    const uint32_t from = plan.own_unit[lane], to = plan.own_unit[lane + 1];
+    const int seq = __builtin_amdgcn_readfirstlane((int)plan.member[j]), rank = __builtin_amdgcn_readfirstlane((int)plan.rank[j]);
     const int at = __popcll(__ballot(lane < plan.n_groups && (int)(lanes.first & 0xffffu) <= j)) - 1;
-    const uint32_t f = lanes.of(lanes.first, at);
-    const int first = (int)(f & 0xffffu), end = at + 1 < 64 ? (int)(lanes.of(lanes.first, at + 1) & 0xffffu) : (int)(plan.g[64].first & 0xffffu);
-    const int blocks = (int)lanes.of(lanes.blocks, at), parts = blocks > 0 ? (int)lanes.of(lanes.parts, at) : 0;
-    const int seq = plan.member[j], kvh = hq / d.g, head = hq - kvh * d.g;
-    const int L = ctx_clamped(d, seq), n_pages = (L + T - 1) / T;
-    const bool missing = blocks > 0 && PKV_CONST(int32_t, d.row_len)[f >> 16] < blocks;
+    const uint32_t f = lanes.of(lanes.first, at), b = lanes.of(lanes.blocks, at);
+    const int first = (int)(f & 0xffffu), blocks = (int)(b & 0xffffffu), parts = (int)(b >> 24);
+    const int kvh = hq / d.g, head = hq - kvh * d.g;
+    const int there = PKV_CONST(int32_t, d.row_len)[f >> 16];
     // where its column is in a part of the prefix
-    const int tile_tok = d.cols / d.g, size = PF_WAVES * tile_tok, count = end - first, wide = (count + size - 1) / size;
-    const int tiles = (count < size ? count + tile_tok - 1 : size) / tile_tok, i = j - first, xg = i / size, in = i - xg * size, w = in / tile_tok;
-    const size_t tile0 = (size_t)lanes.of(lanes.tile, at) + (size_t)(xg * d.Hkv + kvh) * tiles + w, step = (size_t)wide * d.Hkv * tiles;
+    const GroupShape shape(d, lanes.first_member(plan, at + 1) - first);
+    const int tile_tok = d.cols / d.g, i = j - first, xg = i / shape.size, in = i - xg * shape.size, w = in / tile_tok;
+    const size_t tile0 = (size_t)lanes.of(lanes.tile, at) + (size_t)(xg * d.Hkv + kvh) * shape.tiles + w;
     const float *prefix = d.ws + (tile0 * PF_COLS + (in - w * tile_tok) * d.g + head) * (D + 4);
-    const size_t prefix_step = step * PF_COLS * (D + 4);
-    // its own parts (attn_part)
-    int part_pages = d.part_pages;
-    if (n_pages > d.parts * part_pages) part_pages = ((n_pages + d.parts - 1) / d.parts + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES) * (2 * SMALL_WAVES);
-    const int own_parts = n_pages > part_pages ? (n_pages + part_pages - 1) / part_pages : 1;
-    const int pf = partial_floats(d.g, D), all = parts + own_parts;
-    const float *own = plan.own_ws + (size_t)(seq * d.Hkv + kvh) * d.parts * pf;
+    const size_t prefix_step = (size_t)shape.wide * d.Hkv * shape.tiles * PF_COLS * (D + 4);
+    const int own_parts = __popcll(__ballot(to - from > (uint32_t)rank)), pf = partial_floats(d.g, D), all = parts + own_parts;
+    auto own_part = [&](uint32_t k_from) __attribute__((always_inline)) {
+        return plan.own_ws + ((size_t)(k_from + (uint32_t)rank) * d.Hkv + kvh) * pf;
+    };
 
-    float m[2], l[2], M = -INFINITY, den = 0.f;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int p = lane + 64 * k;
-        const float *mp = p < parts ? prefix + p * prefix_step + D : own + (size_t)(p < all ? p - parts : 0) * pf + d.g * D + head;
-        m[k] = p < all ? mp[0] : -INFINITY;
-        l[k] = p < all ? mp[p < parts ? 1 : d.g] : 0.f;
-        M = fmaxf(M, m[k]);
+    float m[2], l[2];
+    {
+        const float *p = prefix + (lane < parts ? lane : 0) * prefix_step + D, *o = own_part(lane < own_parts ? from : lanes.of(from, 0)) + d.g * D + head;
+        m[0] = l[0] = 0.f;
+        if (parts > 0) {
+            m[0] = p[0];
+            l[0] = p[1];
+        }
+        m[1] = o[0];
+        l[1] = o[d.g];
     }
+    const int quad = lane % QUADS, side = lane / QUADS;
+    f32x4 v[TRIP];
+    auto sums = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < TRIP; ++k) {
+            int p = p0 + SIDE * k + side;
+            p = p < all ? p : all - 1;
+            const uint32_t k_from = (uint32_t)__shfl((int)from, p < parts ? 0 : p - parts);
+            const float *src = p < parts ? prefix + p * prefix_step : own_part(k_from) + head * D;
+            v[k] = *reinterpret_cast<const f32x4 *>(src + 4 * quad);
+        }
+    };
+    sums(0);
+    m[0] = lane < parts ? m[0] : -INFINITY;
+    m[1] = lane < own_parts ? m[1] : -INFINITY;
+    float M = fmaxf(m[0], m[1]), den = 0.f;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         m[k] = merge_weight(m[k], M);
-        den += l[k] * m[k];
+        den += m[k] != 0.f ? l[k] * m[k] : 0.f;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
-    const int quad = lane % QUADS, side = lane / QUADS;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < all; p0 += 8 * SIDE) {
-        f32x4 v[8];
+    for (int p0 = 0; p0 < all; p0 += TRIP * SIDE) {
+        if (p0 > 0) sums(p0);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            int p = p0 + SIDE * k + side;
-            p = p < all ? p : all - 1;
-            v[k] = *reinterpret_cast<const f32x4 *>((p < parts ? prefix + p * prefix_step : own + (size_t)(p - parts) * pf + head * D) + 4 * quad);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < TRIP; ++k) {
             const int p = p0 + SIDE * k + side;
-            const float a = __shfl(m[0], p & 63), b = __shfl(m[1], p & 63);
-            if (p < all) acc += v[k] * (p < 64 ? a : b);
+            const float a = __shfl(m[0], p & 63), c = __shfl(m[1], (p - parts) & 63), weight = p < parts ? a : (p < all ? c : 0.f);
+            if (weight != 0.f) acc += v[k] * weight;       // (what weighs nothing may not have been written)
         }
     }
 #pragma unroll
@@ -151,33 +187,30 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
     // a row that sees nothing is defined as zero, and so is one whose prefix is not there
-    const float inv = den > 0.f && !missing ? 1.0f / den : (den != den ? den : 0.f);
-    if (missing) acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (side == 0) *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + hq) * D + 4 * quad) = acc * (missing ? 0.f : inv);
+    if (!(den != 0.f) || there < blocks) {
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        den = 1.f;
+    }
+    if (side == 0) *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + hq) * D + 4 * quad) = acc * (1.0f / den);
+}
+
+template <int D, int DT, int MEET>
+void launch(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s) {
+    static_assert(sizeof(AttnDesc) + sizeof(PrefixPlan) <= 4096, "a kernel's arguments end at 4 KB");
+    static_assert(sizeof(AttnDesc) + sizeof(PlanOf<PKV_PLAN_FEW>) + sizeof(SharedRows) <= 4096, "a kernel's arguments end at 4 KB");
+    hipLaunchKernelGGL((k_prefix_sums<D, DT, MEET>), dim3(plan.prefix_wgs + plan.own_unit[PKV_PLAN_MAX_PARTS] * (unsigned)d.Hkv), dim3(64 * PF_WAVES), 0, s, d, plan);
+    hipLaunchKernelGGL(k_prefix_join<D>, dim3(((unsigned)plan.n_members * (unsigned)d.Hq + JOIN_WAVES - 1) / JOIN_WAVES), dim3(64 * JOIN_WAVES), 0, s, d, plan);
 }
 
 }  // namespace
 
-hipError_t pkv_launch_prefix_sums(const AttnDesc &d, const PrefixPlan &plan, unsigned own_wgs, hipStream_t s) {
-    static_assert(sizeof(AttnDesc) + sizeof(PrefixPlan) <= 4096, "a kernel's arguments end at 4 KB");
-    static_assert(sizeof(AttnDesc) + sizeof(PlanOf<PKV_PLAN_FEW>) + sizeof(SharedRows) <= 4096, "a kernel's arguments end at 4 KB");
-    const dim3 grid(plan.prefix_wgs + own_wgs), wg(64 * PF_WAVES);
-    if (grid.x == 0) return hipSuccess;
+hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s) {
     if (d.dtype == PKV_BF16) {
-        if (d.D == 128) hipLaunchKernelGGL((k_prefix_sums<128, PKV_BF16, 2>), grid, wg, 0, s, d, plan);
-        else hipLaunchKernelGGL((k_prefix_sums<64, PKV_BF16, 2>), grid, wg, 0, s, d, plan);
+        if (d.D == 128) launch<128, PKV_BF16, 2>(d, plan, s);
+        else launch<64, PKV_BF16, 2>(d, plan, s);
     } else {
-        if (d.D == 128) hipLaunchKernelGGL((k_prefix_sums<128, PKV_E4M3, 4>), grid, wg, 0, s, d, plan);
-        else hipLaunchKernelGGL((k_prefix_sums<64, PKV_E4M3, 4>), grid, wg, 0, s, d, plan);
+        if (d.D == 128) launch<128, PKV_E4M3, 4>(d, plan, s);
+        else launch<64, PKV_E4M3, 4>(d, plan, s);
     }
-    return hipGetLastError();
-}
-
-hipError_t pkv_launch_prefix_join(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s) {
-    const unsigned waves = (unsigned)plan.n_members * (unsigned)d.Hq;
-    if (waves == 0) return hipSuccess;
-    const dim3 grid((waves + JOIN_WAVES - 1) / JOIN_WAVES), wg(64 * JOIN_WAVES);
-    if (d.D == 128) hipLaunchKernelGGL(k_prefix_join<128>, grid, wg, 0, s, d, plan);
-    else hipLaunchKernelGGL(k_prefix_join<64>, grid, wg, 0, s, d, plan);
     return hipGetLastError();
 }
