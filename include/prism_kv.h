@@ -277,7 +277,7 @@ int rotary_destroy(int rotary);
  *   q, k, v     dev, bf16; a token's q_heads (kv_heads) heads of head_dim elements lie side by side,
  *               and tokens are *_stride elements apart (0: packed), so all three may be parts of
  *               one fused projection.  16-byte aligned rows are read faster; any alignment works.
- *   q_weight, k_weight   dev, bf16 [head_dim], or NULL: that one is not normed
+ *   q_weight, k_weight   dev, bf16 [head_dim], 16-byte aligned, or NULL: that one is not normed
  *   rotary      an id of rotary_create with rot_dim <= head_dim (PKV_E_SHAPE), or -1: no rotation
  *   before      dev int32 [batch], or NULL (zeros): tokens in front of the row's first one, e.g. those
  *               of a shared prefix: token j of row s stands at position before[s] + j

@@ -175,6 +175,7 @@ class PrismKV:
         self.lib = _load()
         self._shape = {}
         self._keep = {}
+        self._qkv_args = _Qkv()                    # (the call reads it before it returns)
         self.use_current_stream()
 
     # ---- host policies (no GPU work)
@@ -405,25 +406,32 @@ class PrismKV:
 
     def _qkv(self, model, q, k, v, q_weight, k_weight, eps, rotary, before):
         hq, hkv, d, _ = self._shape[model]
+        args = self._qkv_args
         strides = []
         for x, heads in ((q, hq), (k, hkv), (v, hkv)):
             # a token's heads side by side, tokens any distance apart
-            assert x.dim() == 3 and tuple(x.shape[1:]) == (heads, d) and x.element_size() == 2
-            assert x.stride(2) == 1 and (heads == 1 or x.stride(1) == d)
-            strides.append(x.stride(0) if x.shape[0] > 1 else 0)
-        a = lambda t: None if t is None else t.data_ptr()
-        return _Qkv(a(q), a(k), a(v), *strides, a(q_weight), a(k_weight), eps, rotary, a(before))
+            shape, stride = x.shape, x.stride()
+            assert len(shape) == 3 and shape[1] == heads and shape[2] == d and x.element_size() == 2
+            assert stride[2] == 1 and (heads == 1 or stride[1] == d)
+            strides.append(stride[0] if shape[0] > 1 else 0)
+        args.q, args.k, args.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+        args.q_stride, args.k_stride, args.v_stride = strides
+        args.q_weight = None if q_weight is None else q_weight.data_ptr()
+        args.k_weight = None if k_weight is None else k_weight.data_ptr()
+        args.before = None if before is None else before.data_ptr()
+        args.eps, args.rotary = eps, rotary
+        return C.byref(args)
 
     def qkv_append_dev(self, model, q, k, v, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues."""
         x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append(model, ctx_lens.numel(), C.byref(x), self._p(ctx_lens), self._p(q_out))
+        return self.lib.qkv_append(model, ctx_lens.numel(), x, self._p(ctx_lens), self._p(q_out))
 
     def qkv_append_chunk_dev(self, model, q, k, v, q_lens, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """The same for packed chunks; q_lens: host int32 numpy array.  Only enqueues."""
         q_lens = np.ascontiguousarray(q_lens, dtype=np.int32)
         x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append_chunk(model, q_lens.size, C.byref(x), q_lens.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(q_out))
+        return self.lib.qkv_append_chunk(model, q_lens.size, x, q_lens.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(q_out))
 
     def kv_read(self, model, seq, tok_begin, n_tok):
         """-> (code, k, v, k_scale, v_scale) as numpy: elements [n_tok][Hkv][D], scales [n_tok][Hkv] (None for bf16)."""

@@ -194,7 +194,7 @@ struct AsTheyAre {
 
 // bf16 values into a bf16 tile
 template <int D, bool IS_V, typename TILE_OF, typename TURN>
-__device__ __forceinline__ void page_bf16(const TILE_OF &tile_of, const PageRows &p, TURN &turn) {
+__device__ __forceinline__ void page_bf16(const TILE_OF &tile_of, const PageRows &p, TURN &&turn) {
     const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4, G = t >> 2, e = t & 3;
     uint32_t w[D / 32][4];
     read_rows(p, [&](auto a) __attribute__((always_inline)) {
@@ -338,7 +338,7 @@ __device__ __forceinline__ uint32_t lower_codes(uint32_t w, uint32_t lo, uint32_
 constexpr int FEW_LANES = 4;
 
 template <int D, bool IS_V, typename TILE_OF, typename TURN>
-__device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const PageRows &p, TURN &turn) {
+__device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const PageRows &p, TURN &&turn) {
     constexpr int NW = D / 16;                           // words of codes per lane
     const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4, G = t >> 2, e = t & 3;
     const int s0 = p.s0, end = p.s0 + p.n;
@@ -529,14 +529,9 @@ __device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const Page
 }
 
 // One wave's share of a page: the K (which = 0) or V (1) tile of kv head h.  QUANT: bf16 values into an e4m3 block.
-// block_of(): the block, or NULL where nothing may be written.  turn_of: what makes what is done to K rows, by the head's width.
-struct NoTurn {
-    template <int D>
-    __device__ __forceinline__ AsTheyAre of() const { return AsTheyAre{}; }
-};
-template <int DT, bool QUANT, typename BLOCK_OF, typename TURN_OF = NoTurn>
-__device__ __forceinline__ void page_tile(const AttnDesc &d, const BLOCK_OF &block_of, int h, int which, const PageRows &p,
-                                          const TURN_OF &turn_of = TURN_OF{}) {
+// block_of(): the block, or NULL where nothing may be written.
+template <int DT, bool QUANT, typename BLOCK_OF>
+__device__ __forceinline__ void page_tile(const AttnDesc &d, const BLOCK_OF &block_of, int h, int which, const PageRows &p) {
     constexpr int E = DT == PKV_BF16 ? 2 : 1;
     const size_t offset = (DT == PKV_E4M3 ? PKV_FP8_HEADER : 0) + ((size_t)h * 2 + which) * PKV_T * d.D * E;
     auto go = [&](auto dim, auto is_v) __attribute__((always_inline)) {
@@ -546,7 +541,7 @@ __device__ __forceinline__ void page_tile(const AttnDesc &d, const BLOCK_OF &blo
             uint8_t *blk = block_of();
             return blk ? blk + offset : blk;
         };
-        auto turn = turn_of.template of<D>();
+        AsTheyAre turn;
         if constexpr (DT == PKV_BF16) page_bf16<D, IS_V>(tile_of, p, turn);
         else if constexpr (!QUANT) page_codes<D, IS_V>(tile_of, p);
         else

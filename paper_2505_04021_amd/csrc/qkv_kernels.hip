@@ -43,42 +43,6 @@ __device__ __forceinline__ int partner_of(const QkvArgs &a, int e) {
     return e < half ? e + half : e - half;
 }
 
-// Eight elements e0 .. e0 + 7 of a head: factors of the element itself and of its partner (rotated elements only).
-__device__ __forceinline__ void factors(const QkvArgs &a, int e0, int pos, float *cs, float *sn) {
-    if (!a.turns) return;
-    const int half = a.rot >> 1;
-    if (a.pairs) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int pair = (e0 >> 1) + i;
-            float s, c;
-            turn_of(a.turns[pair < half ? pair : 0], pos, s, c);
-            cs[2 * i] = cs[2 * i + 1] = c * a.magnitude;
-            sn[2 * i + 1] = s * a.magnitude;
-            sn[2 * i] = -sn[2 * i + 1];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = e0 + i, pair = e < half ? e : (e < a.rot ? e - half : 0);
-            float s, c;
-            turn_of(a.turns[pair], pos, s, c);
-            cs[i] = c * a.magnitude;
-            sn[i] = (e < half ? -s : s) * a.magnitude;
-        }
-    }
-}
-
-// Eight elements turned; px: their partners, of the half layout only.
-__device__ __forceinline__ void turn8(const QkvArgs &a, int e0, float *x, const float *px, const float *cs, const float *sn) {
-    if (!a.turns) return;
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i] * cs[i] + (a.pairs ? x[i ^ 1] : px[i]) * sn[i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = e0 + i < a.rot ? y[i] : x[i];
-}
-
 __device__ __forceinline__ float lanes4_sum(float x) {    // over lanes l, l ^ 16, l ^ 32, l ^ 48
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
@@ -96,150 +60,274 @@ __device__ __forceinline__ float head_sum(float x) {      // over the 8 or 16 la
     return x;
 }
 
-// The keys of a page on their way into its tile (kv_pages.h).  pos: the position of slot 0's token.
-template <int D>
-struct TurnKeys {
-    const QkvArgs &a;
-    const int pos0;
-    int t, c;
-    uint32_t px[D / 32][4];                               // the partners of this lane's elements, half layout
+__device__ __forceinline__ float square_sum(const uint32_t *w) {
+    float x[8], sum = 0.f;
+    widen(x, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+    return sum;
+}
+__device__ __forceinline__ float norm_of(float squares, int width, float eps) { return __builtin_amdgcn_rsqf(squares / (float)width + eps); }
 
-    __device__ __forceinline__ TurnKeys(const QkvArgs &args, int pos) : a(args), pos0(pos) {}
+// What makes eight elements e0 .. e0 + 7 of a head's outcome at a position: x own + partner other, with the norm's weights and the magnitude in
+// it, the same for all heads.  An element that is not rotated has no partner: other = -0, and its partner is taken as 0, so that it stays
+// what it is, an infinity and a zero's sign too.
+struct Factors {
+    float own[8], other[8];
+};
+__device__ __forceinline__ void eight_weights(float *w, const uint16_t *weight, int e0) {
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(weight + e0);
+    const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+    widen(w, words);
+}
+// The turns of N pairs in a row (the table has 64 entries, whatever the rotation).
+template <int N>
+__device__ __forceinline__ void some_turns(uint64_t *t, const QkvArgs &a, int pair) {
+    typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const u64x2 v = *reinterpret_cast<const u64x2 *>(a.turns + pair + i);
+        t[i] = v.x;
+        t[i + 1] = v.y;
+    }
+}
 
-    __device__ __forceinline__ void ask(const PageRows &p, int slot, int col) {
-        t = slot;
-        c = col;
-        const int half = a.rot >> 1;
-        if (!a.turns || a.pairs) {
+template <bool PAIRS>
+__device__ __forceinline__ Factors factors(const QkvArgs &a, const uint16_t *weight, int e0, int pos, bool rotated) {
+    Factors f;
+    const int half = a.rot >> 1;
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
+    for (int i = 0; i < 8; ++i) {
+        f.own[i] = 1.f;
+        f.other[i] = -0.f;
+    }
+    if (weight) eight_weights(f.own, weight, e0);
+    if (!rotated) return f;
+    uint64_t turns[8];
+    float pw[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) px[j][i] = 0u;
-        } else if (p.aligned && (half & 7) == 0) {
+    for (int i = 0; i < 8; ++i) pw[i] = 1.f;
+    if constexpr (PAIRS) some_turns<4>(turns, a, e0 >> 1);
+    else if ((half & 7) == 0) {                            // a group's partners are a group
+        const int low = (e0 < half ? e0 : e0 - half) & 63;
+        some_turns<8>(turns, a, low);
+        if (weight) eight_weights(pw, weight, partner_of(a, e0));
+    } else {
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) row_bytes<16, 2, true>(px[j], p, t, 2 * partner_of(a, 8 * (4 * j + c)));
-        } else {
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t w[1];
-                    const int at = partner_of(a, 8 * (4 * j + c) + i);
-                    row_bytes<4, 2, false>(w, p, t, 2 * (at & ~1));
-                    const uint32_t b = (at & 1) ? w[0] >> 16 : w[0] & 0xffffu;
-                    px[j][i >> 1] = (i & 1) ? px[j][i >> 1] | b << 16 : b;
-                }
+        for (int i = 0; i < 8; ++i) {
+            const int e = e0 + i;
+            turns[i] = a.turns[(e < half ? e : e - half) & 63];
+            if (weight) pw[i] = bf16_of(weight[partner_of(a, e)]);
         }
     }
+#pragma unroll
+    for (int i = 0; i < 8; i += PAIRS ? 2 : 1) {
+        const int e = e0 + i;
+        const bool in = e < a.rot;                         // (rot is even: neighbours are rotated or not together)
+        float sn, cs;
+        turn_of(turns[PAIRS ? i >> 1 : i], pos, sn, cs);
+        sn *= a.magnitude;
+        cs *= a.magnitude;
+        if constexpr (PAIRS) {
+            const float o0 = -sn * f.own[i + 1], o1 = sn * f.own[i];
+            f.other[i] = in ? o0 : -0.f;
+            f.other[i + 1] = in ? o1 : -0.f;
+            f.own[i] *= in ? cs : 1.f;
+            f.own[i + 1] *= in ? cs : 1.f;
+        } else {
+            const float o = (e < half ? -sn : sn) * pw[i];
+            f.other[i] = in ? o : -0.f;
+            f.own[i] *= in ? cs : 1.f;
+        }
+    }
+    return f;
+}
 
+// Eight elements' outcome.  xw: their words, pw: their partners' (0 where there is none; not looked at for pairs of neighbours, whose
+// partners are among them); r: the head's norm, 1 without one.
+template <bool PAIRS>
+__device__ __forceinline__ u32x4 turned8(const Factors &f, const uint32_t *xw, const uint32_t *pw, int e0, int rot, float r) {
+    float x[8], p[8], y[8];
+    widen(x, xw);
+    if constexpr (PAIRS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = e0 + i < rot ? x[i ^ 1] : 0.f;
+    } else widen(p, pw);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (x[i] * r) * f.own[i] + (p[i] * r) * f.other[i];
+    return mk4(pack_bf16_rne(y[0], y[1]), pack_bf16_rne(y[2], y[3]), pack_bf16_rne(y[4], y[5]), pack_bf16_rne(y[6], y[7]));
+}
+
+// The eight partners of elements e0 .. e0 + 7 by elements, 0 where there is none.
+__device__ __forceinline__ void partners_by_element(const QkvArgs &a, const uint16_t *row, int e0, uint32_t *pw) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = e0 + 2 * i;
+        const uint32_t lo = row[partner_of(a, e)], hi = row[partner_of(a, e + 1)];
+        pw[i] = (e < a.rot ? lo : 0u) | (e + 1 < a.rot ? hi << 16 : 0u);
+    }
+}
+
+// The keys of a page on their way into its tile (kv_pages.h).  A lane holds every fourth group of eight elements of its token, so that with half
+// layout's partners 32 or 64 elements away it holds both (`near`) and works each angle out once; others are read.  (Factors kept in registers
+// for several heads of a page: 237 registers, two waves a SIMD for the queries too.)
+template <int D, bool PAIRS>
+struct TurnKeys {
+    const QkvArgs &a;
+    const int pos, c;                                     // this lane's token and column group
+    const bool near;
+    uint32_t px[D / 32][4];
+
+    __device__ __forceinline__ TurnKeys(const QkvArgs &args, int pos) : a(args), pos(pos), c((int)(threadIdx.x & 63) >> 4), near((args.rot >> 1 & 31) == 0) {}
+    __device__ __forceinline__ void ask(const PageRows &p, int t, int) {
+        if (PAIRS || near) return;
+        int r = t - p.s0;
+        r = r < 0 ? 0 : (r < p.n ? r : p.n - 1);
+        const uint16_t *row = reinterpret_cast<const uint16_t *>(p.src + (size_t)r * p.stride);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            const int e0 = 8 * (4 * j + c);
+            if (p.aligned && (a.rot >> 1 & 7) == 0) {
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(row + partner_of(a, e0));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) px[j][i] = e0 < a.rot ? v[i] : 0u;
+            } else partners_by_element(a, row, e0, px[j]);
+        }
+    }
+    // groups j and k, pairs 8 (4 j + c) .. + 7: both outcomes
+    __device__ __forceinline__ void both(uint32_t *words, int j, int k, float r) {
+        const int e0 = 8 * (4 * j + c), e1 = 8 * (4 * k + c);
+        float x[8], y[8], u[8], v[8], wx[8], wy[8];
+        widen(x, words + 4 * j);
+        widen(y, words + 4 * k);
+        uint64_t turns[8];
+        some_turns<8>(turns, a, e0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wx[i] = wy[i] = 1.f;
+        if (a.k_weight) {
+            eight_weights(wx, a.k_weight, e0);
+            eight_weights(wy, a.k_weight, e1);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float sn, cs;
+            turn_of(turns[i], pos, sn, cs);
+            const float p = (x[i] * r) * wx[i], q = (y[i] * r) * wy[i];
+            sn *= a.magnitude;
+            cs *= a.magnitude;
+            u[i] = p * cs - q * sn;
+            v[i] = q * cs + p * sn;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            words[4 * j + i] = pack_bf16_rne(u[2 * i], u[2 * i + 1]);
+            words[4 * k + i] = pack_bf16_rne(v[2 * i], v[2 * i + 1]);
+        }
+    }
     __device__ __forceinline__ void turn(uint32_t *words) {
+        if (!a.turns && !a.k_weight) return;
         float r = 1.f;
         if (a.k_weight) {
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-                float x[8];
-                widen(x, words + 4 * j);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-            }
-            r = 1.0f / sqrtf(lanes4_sum(sum) * (1.0f / D) + a.eps);
+            for (int j = 0; j < D / 32; ++j) sum += square_sum(words + 4 * j);
+            r = norm_of(lanes4_sum(sum), D, a.eps);
         }
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
+        auto group = [&](int j, bool rotated) __attribute__((always_inline)) {
             const int e0 = 8 * (4 * j + c);
-            float x[8], p[8], cs[8], sn[8];
-            widen(x, words + 4 * j);
-            widen(p, px[j]);
-            if (a.k_weight) {
+            uint32_t none[4] = {0u, 0u, 0u, 0u};
+            const Factors f = factors<PAIRS>(a, a.k_weight, e0, pos, rotated);
+            const u32x4 y = turned8<PAIRS>(f, words + 4 * j, rotated && !PAIRS ? px[j] : none, e0, a.rot, r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] *= r * bf16_of(a.k_weight[e0 + i]);
-                    p[i] *= r * bf16_of(a.k_weight[partner_of(a, e0 + i)]);
+            for (int i = 0; i < 4; ++i) words[4 * j + i] = y[i];
+        };
+        if (!PAIRS && a.turns && near) {
+            if (D == 128 && a.rot == 128) {
+                both(words, 0, D == 128 ? 2 : 1, r);
+                both(words, 1, D == 128 ? 3 : 1, r);
+            } else {                                       // rot = 64
+                both(words, 0, 1, r);
+                if (D == 128 && a.k_weight) {
+#pragma unroll
+                    for (int j = 2; j < D / 32; ++j) group(j, false);
                 }
             }
-            factors(a, e0, pos0 + t, cs, sn);
-            turn8(a, e0, x, p, cs, sn);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) words[4 * j + i] = pack_bf16_rne(x[2 * i], x[2 * i + 1]);
+            return;
         }
+        // (a condition for the whole wave: lanes of one group of eight differ in it only where rot is no multiple of 32)
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) group(j, a.turns && 32 * j < a.rot);
     }
 };
 
-struct TurnKeysOf {
-    const QkvArgs &a;
-    int pos;
-    template <int D>
-    __device__ __forceinline__ TurnKeys<D> of() const { return TurnKeys<D>(a, pos); }
-};
-
-// Heads head0 .. head0 + heads - 1 of one token's query, 8 elements a lane, 64 * 8 / D heads at a time: read, normed, turned and written
-// as whole rows of 16-byte pieces.  The angles are worked out once for all heads.
-template <int D>
-__device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a, int64_t row, int pos, int head0, int heads) {
-    constexpr int LANES = D / 8, ROWS = 64 / LANES;
+// Heads head0 .. head0 + heads - 1 of one token's query, 8 elements a lane, 512 / D heads at a time: whole rows of 16-byte pieces.  The
+// first rows are asked for ahead of the token's position (pos_of()), the next ones ahead of the arithmetic of those before.
+template <int D, bool PAIRS, typename POS_OF>
+__device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a, int64_t row, int head0, int heads, const POS_OF &pos_of) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, BATCH = 4;
     const int lane = threadIdx.x & 63, c = lane % LANES, e0 = 8 * c, half = a.rot >> 1;
-    const bool halves = a.turns && !a.pairs, whole = a.q_aligned && (half & 7) == 0;
-    float cs[8], sn[8], w[8], pw[8];
-    factors(a, e0, pos, cs, sn);
-    if (a.q_weight) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w[i] = bf16_of(a.q_weight[e0 + i]);
-            pw[i] = bf16_of(a.q_weight[partner_of(a, e0 + i)]);
-        }
-    }
-    const int from = lane - c + (halves ? partner_of(a, e0) >> 3 : c);       // where whole partners are
     const uint16_t *src = a.q + row * a.q_stride;
     uint16_t *dst = a.q_out + row * d.Hq * D;
-    for (int h0 = head0; h0 < head0 + heads; h0 += ROWS) {
-        const int h = h0 + lane / LANES;
-        const bool live = h < head0 + heads;
-        const uint16_t *x_at = src + (live ? h : head0) * D;
-        uint32_t xw[4], pxw[4];
-        if (a.q_aligned) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(x_at + e0);
+    auto head_of = [&](int h0) __attribute__((always_inline)) { return h0 + lane / LANES; };
+    auto load = [&](u32x4 *x, int h0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) xw[i] = v[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) xw[i] = x_at[e0 + 2 * i] | (uint32_t)x_at[e0 + 2 * i + 1] << 16;
+        for (int k = 0; k < BATCH; ++k) {
+            const int h = head_of(h0 + k * ROWS);
+            const uint16_t *at = src + (h < head0 + heads ? h : head0) * D + e0;
+            if (a.q_aligned) x[k] = *reinterpret_cast<const u32x4 *>(at);
+            else x[k] = mk4(at[0] | (uint32_t)at[1] << 16, at[2] | (uint32_t)at[3] << 16, at[4] | (uint32_t)at[5] << 16, at[6] | (uint32_t)at[7] << 16);
         }
-        if (halves && whole) {
+        asked_for();
+    };
+    u32x4 x[BATCH], next[BATCH];
+    load(x, head0);
+    const Factors f = factors<PAIRS>(a, a.q_weight, e0, pos_of(), a.turns != nullptr);
+    const bool whole = (half & 7) == 0;                   // a group's partners are a group
+    const int from = lane - c + (!PAIRS && whole ? partner_of(a, e0) >> 3 : c);
+    for (int h0 = head0; h0 < head0 + heads; h0 += BATCH * ROWS) {
+        const bool more = h0 + BATCH * ROWS < head0 + heads;
+        if (more) load(next, h0 + BATCH * ROWS);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pxw[i] = (uint32_t)__shfl((int)xw[i], from);
-        } else if (halves) {
+        for (int k = 0; k < BATCH; ++k) {
+            if (h0 + k * ROWS >= head0 + heads) break;
+            const int h = head_of(h0 + k * ROWS);
+            const bool live = h < head0 + heads;
+            uint32_t xw[4], pw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pxw[i] = x_at[partner_of(a, e0 + 2 * i)] | (uint32_t)x_at[partner_of(a, e0 + 2 * i + 1)] << 16;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pxw[i] = 0u;
-        }
-        float x[8], p[8];
-        widen(x, xw);
-        widen(p, pxw);
-        if (a.q_weight) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-            const float r = 1.0f / sqrtf(head_sum<LANES>(sum) * (1.0f / D) + a.eps);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] *= r * w[i];
-                p[i] *= r * pw[i];
+            for (int i = 0; i < 4; ++i) {
+                xw[i] = x[k][i];
+                pw[i] = 0u;
             }
+            if (!PAIRS && a.turns) {
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t w = (uint32_t)__shfl((int)xw[i], from);
+                        pw[i] = e0 < a.rot ? w : 0u;
+                    }
+                } else partners_by_element(a, src + (live ? h : head0) * D, e0, pw);
+            }
+            const float r = a.q_weight ? norm_of(head_sum<LANES>(square_sum(xw)), D, a.eps) : 1.f;
+            const u32x4 y = turned8<PAIRS>(f, xw, pw, e0, a.rot, r);
+            if (live) *reinterpret_cast<u32x4 *>(dst + h * D + e0) = y;
         }
-        turn8(a, e0, x, p, cs, sn);
-        if (live)
-            *reinterpret_cast<u32x4 *>(dst + h * D + e0) =
-                mk4(pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3]), pack_bf16_rne(x[4], x[5]), pack_bf16_rne(x[6], x[7]));
+        if (more) {
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) x[k] = next[k];
+        }
     }
 }
 
-__device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a, int64_t row, int pos, int head0) {
+template <typename POS_OF>
+__device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a, int64_t row, int head0, const POS_OF &pos_of) {
     const int heads = d.Hq - head0 < a.wave_heads ? d.Hq - head0 : a.wave_heads;
-    if (d.D == 128) turn_queries<128>(d, a, row, pos, head0, heads);
-    else turn_queries<64>(d, a, row, pos, head0, heads);
+    if (d.D == 128) {
+        if (a.pairs) turn_queries<128, true>(d, a, row, head0, heads, pos_of);
+        else turn_queries<128, false>(d, a, row, head0, heads, pos_of);
+    } else {
+        if (a.pairs) turn_queries<64, true>(d, a, row, head0, heads, pos_of);
+        else turn_queries<64, false>(d, a, row, head0, heads, pos_of);
+    }
 }
 
 // The decode step.  One wave per (sequence, kv head) for K and V of its new token, the element layout of k_kv_append, then
@@ -249,8 +337,9 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
     const int lane = threadIdx.x, D = d.D, kv_waves = d.batch * d.Hkv;
     if ((int)blockIdx.x >= kv_waves) {
         const int x = blockIdx.x - kv_waves, per = (d.Hq + a.wave_heads - 1) / a.wave_heads, seq = x / per;
-        const int before = a.before ? PKV_CONST(int32_t, a.before)[seq] : 0;
-        turn_queries(d, a, seq, before + PKV_CONST(int32_t, d.ctx_lens)[seq] - 1, (x - seq * per) * a.wave_heads);
+        turn_queries(d, a, seq, (x - seq * per) * a.wave_heads, [&]() __attribute__((always_inline)) {
+            return (a.before ? PKV_CONST(int32_t, a.before)[seq] : 0) + PKV_CONST(int32_t, d.ctx_lens)[seq] - 1;
+        });
         return;
     }
     const int seq = blockIdx.x / d.Hkv, h = blockIdx.x - seq * d.Hkv;
@@ -275,7 +364,7 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
             float sum = x[0] * x[0] + (D > 64 ? x[1] * x[1] : 0.f);
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            r = 1.0f / sqrtf(sum / (float)D + a.eps);
+            r = norm_of(sum, D, a.eps);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -317,31 +406,36 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
     }
 }
 
-// A prefill chunk.  Waves of whole pages as in k_kv_append_chunk (one per page the chunk touches, kv head, and K or V), then waves for
+// Bound by memory: ragged prompts of 4300 tokens of 32/8/128, neighbours as pairs, 115 MB, cold: 27.1 us (22.6 at a large copy's rate; 25.8 with
+// neither norm nor rotation).  39.0 with every head's weights and angles looked up and worked out by themselves, one row in flight a wave;
+// with registers for five waves a SIMD instead of four 32.4, for three 28.9.  2400 tokens into an e4m3 cache 14.5 (before 23.5).
+// A prefill chunk.  Waves of whole pages as in k_kv_append_chunk (one per page that the chunk touches, kv head, and K or V), then waves for
 // the queries, each with some heads of one token.
 constexpr int QKV_WAVES = 4;
 
-template <int DT, int SEQS>
-__global__ __launch_bounds__(64 * QKV_WAVES) void k_qkv_append_chunk(const AttnDesc d, const QkvArgs a, const PlanOf<SEQS> plan) {
+template <int D, int DT, int SEQS>
+__global__ __launch_bounds__(64 * QKV_WAVES, 4) void k_qkv_append_chunk(const AttnDesc d, const QkvArgs a, const PlanOf<SEQS> plan) {
+    constexpr int E = DT == PKV_BF16 ? 2 : 1;
     const int lane = threadIdx.x & 63;
     const PlanLanes<SEQS> lanes(plan);
     const int n_seqs = plan.n_seqs;
     int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * QKV_WAVES + (threadIdx.x >> 6)));
-    const int kv_waves = (int)lanes.units(plan) * d.Hkv * 2;
-    if (x >= kv_waves) {
-        x -= kv_waves;
+    const int page_waves = (int)lanes.units(plan) * d.Hkv * 2;
+    if (x >= page_waves) {
+        x -= page_waves;
         const int per = (d.Hq + a.wave_heads - 1) / a.wave_heads, row0 = (int)(lanes.pick(lanes.row, 0) & PKV_PLAN_ROWS);
         const int row = row0 + x / per;
         if (row >= (int)(lanes.pick(lanes.row, n_seqs) & PKV_PLAN_ROWS)) return;           // the last work-group may have waves to spare
-        const PlanUnit pu = lanes.find_row(plan, (uint32_t)row);
-        const int before = a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0, ctx = PKV_CONST(int32_t, d.ctx_lens)[pu.seq];
-        turn_queries(d, a, row, before + ctx - pu.rows + row - pu.row, (x % per) * a.wave_heads);
+        turn_queries(d, a, row, (x % per) * a.wave_heads, [&]() __attribute__((always_inline)) {
+            const PlanUnit pu = lanes.find_row(plan, (uint32_t)row);
+            return (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + PKV_CONST(int32_t, d.ctx_lens)[pu.seq] - pu.rows + row - pu.row;
+        });
         return;
     }
-    const int which = x & 1, hp = x >> 1, unit = hp / d.Hkv, h = hp - unit * d.Hkv;
+    const bool keys = (x & 1) == 0;
+    const int unit = (x >> 1) / d.Hkv, h = (x >> 1) - unit * d.Hkv;
     const PlanUnit pu = lanes.find(plan, (uint32_t)unit);
     const int ctx = PKV_CONST(int32_t, d.ctx_lens)[pu.seq], cap = PKV_CONST(int32_t, d.row_len)[pu.seq] * PKV_T;
-    const int before = a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0;
     if ((ctx < pu.rows) | (ctx < 1) | (ctx > cap)) {
         if (lane == 0) atomicOr(d.err, 2u);
         return;
@@ -350,21 +444,44 @@ __global__ __launch_bounds__(64 * QKV_WAVES) void k_qkv_append_chunk(const AttnD
     const int lo = tok0 > page * PKV_T ? tok0 : page * PKV_T, hi = ctx < (page + 1) * PKV_T ? ctx : (page + 1) * PKV_T;
     if (lo >= hi) return;
     const uint32_t id = (uint32_t)PKV_CONST(int32_t, d.table)[(size_t)pu.seq * d.row_stride + page];
-    const uint16_t *src = which ? a.v : a.k;
-    const int64_t stride = which ? a.v_stride : a.k_stride;
+    const uint16_t *src = keys ? a.k : a.v;
+    const int64_t stride = keys ? a.k_stride : a.v_stride;
     PageRows p;
     p.stride = (size_t)stride * 2;
-    p.src = reinterpret_cast<const uint8_t *>(src + (pu.row + (lo - tok0)) * stride + (size_t)h * d.D);
     p.s0 = lo % PKV_T;
     p.n = hi - lo;
     p.aligned = ((reinterpret_cast<uintptr_t>(src) | (uintptr_t)(stride * 2)) & 15) == 0;
-    page_tile<DT, true>(d, [&]() __attribute__((always_inline)) -> uint8_t * {
-        if (id >= d.max_block_id) {
-            if (lane == 0) atomicOr(d.err, 1u);
-            return nullptr;
+    p.src = reinterpret_cast<const uint8_t *>(src + (pu.row + (lo - tok0)) * stride + (size_t)h * D);
+    auto page_of = [&](auto is_v, auto &&turn) __attribute__((always_inline)) {
+        constexpr bool IS_V = decltype(is_v)::value;
+        auto block = [&]() __attribute__((always_inline)) -> uint8_t * {
+            if (id >= d.max_block_id) {
+                if (lane == 0) atomicOr(d.err, 1u);
+                return nullptr;
+            }
+            return block_ptr(d, id);
+        };
+        const size_t offset = (DT == PKV_E4M3 ? PKV_FP8_HEADER : 0) + ((size_t)h * 2 + (IS_V ? 1 : 0)) * PKV_T * D * E;
+        if constexpr (DT == PKV_BF16) {
+            page_bf16<D, IS_V>([&]() __attribute__((always_inline)) -> uint8_t * {
+                uint8_t *blk = block();
+                return blk ? blk + offset : blk;
+            }, p, turn);
+        } else {
+            page_quantise<D, IS_V>([&](float *&scale_p) __attribute__((always_inline)) -> uint8_t * {
+                uint8_t *blk = block();
+                scale_p = reinterpret_cast<float *>(blk) + (IS_V ? d.Hkv : 0) + h;
+                return blk ? blk + offset : blk;
+            }, p, turn);
         }
-        return block_ptr(d, id);
-    }, h, which, p, TurnKeysOf{a, before + page * PKV_T});
+    };
+    if (!keys) {
+        page_of(std::true_type{}, AsTheyAre{});
+        return;
+    }
+    const int pos = (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + page * PKV_T + (lane & 15);
+    if (a.pairs) page_of(std::false_type{}, TurnKeys<D, true>(a, pos));
+    else page_of(std::false_type{}, TurnKeys<D, false>(a, pos));
 }
 
 }  // namespace
@@ -380,13 +497,19 @@ hipError_t pkv_launch_qkv_append(const AttnDesc &d, const QkvArgs &a, hipStream_
 template <int SEQS>
 static void launch_chunk(const AttnDesc &d, const QkvArgs &a, const PlanOf<SEQS> &plan, dim3 grid, hipStream_t s) {
     static_assert(sizeof(AttnDesc) + sizeof(QkvArgs) + sizeof(PlanOf<SEQS>) <= 4096, "a kernel's arguments end at 4 KB");
-    if (d.dtype == PKV_BF16) hipLaunchKernelGGL((k_qkv_append_chunk<PKV_BF16, SEQS>), grid, dim3(64 * QKV_WAVES), 0, s, d, a, plan);
-    else hipLaunchKernelGGL((k_qkv_append_chunk<PKV_E4M3, SEQS>), grid, dim3(64 * QKV_WAVES), 0, s, d, a, plan);
+    const dim3 wg(64 * QKV_WAVES);
+    if (d.dtype == PKV_BF16) {
+        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_BF16, SEQS>), grid, wg, 0, s, d, a, plan);
+        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_BF16, SEQS>), grid, wg, 0, s, d, a, plan);
+    } else {
+        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_E4M3, SEQS>), grid, wg, 0, s, d, a, plan);
+        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_E4M3, SEQS>), grid, wg, 0, s, d, a, plan);
+    }
 }
 
 hipError_t pkv_launch_qkv_append_chunk(const AttnDesc &d, const QkvArgs &a, const ChunkPlan &plan, hipStream_t s) {
-    const uint64_t rows = (plan.s[plan.n_seqs].row & PKV_PLAN_ROWS) - (plan.s[0].row & PKV_PLAN_ROWS);
-    const uint64_t waves = (uint64_t)plan.s[plan.n_seqs].unit * d.Hkv * 2 + rows * ((d.Hq + a.wave_heads - 1) / a.wave_heads);
+    const uint64_t rows = (plan.s[plan.n_seqs].row & PKV_PLAN_ROWS) - (plan.s[0].row & PKV_PLAN_ROWS), units = plan.s[plan.n_seqs].unit;
+    const uint64_t waves = units * (uint64_t)d.Hkv * 2 + rows * (uint64_t)((d.Hq + a.wave_heads - 1) / a.wave_heads);
     if (rows == 0) return hipSuccess;
     if (waves > 0x7fffffffu) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)((waves + QKV_WAVES - 1) / QKV_WAVES));
