@@ -390,8 +390,9 @@ int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens
  * seen.  PKV_E_RANGE where a row is known to hold fewer blocks than are to be shared; where that turns
  * out on the device (bookkeeping enqueued and refused), bit 0 of pkv_device_errors() is raised and the rows
  * of those sequences are zero.  Sums travel through a buffer of the model, made or enlarged when first
- * needed (PKV_E_NOMEM while the stream is being captured: make the call once before the capture); two calls
- * of this section on one model must not overlap in time.  Otherwise they only enqueue.
+ * needed (PKV_E_NOMEM while the stream is being captured: make the call once before the capture), and
+ * small decode steps use the split-K workspace: two calls of this section on one model must not overlap in
+ * time, nor one with a decode_attention* call.  Otherwise they only enqueue.
  *
  * decode_attention_prefix: q dev bf16 [batch][q_heads][head_dim], out [batch][q_heads][head_dim].  Sequences
  * with the same prefix_seqs and prefix_blocks form a group; a group's prefix is read once for all its members,

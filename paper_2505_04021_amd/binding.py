@@ -120,6 +120,12 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
            "kv_gather", "decode_attention_prefix", "prefill_attention_prefix"]
 
 
+def _i32(a):
+    """(array, address) of a host int32 list; the array has to outlive the call."""
+    a = np.ascontiguousarray(a, dtype=np.int32)
+    return a, a.__array_interface__["data"][0]
+
+
 def _f64(a):
     return np.ascontiguousarray(a, dtype=np.float64)
 
@@ -429,9 +435,9 @@ class PrismKV:
 
     def qkv_append_chunk_dev(self, model, q, k, v, q_lens, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """The same for packed chunks; q_lens: host int32 numpy array.  Only enqueues."""
-        q_lens = np.ascontiguousarray(q_lens, dtype=np.int32)
+        ql, ql_at = _i32(q_lens)
         x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append_chunk(model, q_lens.size, x, q_lens.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(q_out))
+        return self.lib.qkv_append_chunk(model, ql.size, x, ql_at, self._p(ctx_lens), self._p(q_out))
 
     def kv_read(self, model, seq, tok_begin, n_tok):
         """-> (code, k, v, k_scale, v_scale) as numpy: elements [n_tok][Hkv][D], scales [n_tok][Hkv] (None for bf16)."""
@@ -453,9 +459,9 @@ class PrismKV:
 
     def kv_gather_dev(self, model, seqs, tok_begin, n_tok, k_out, v_out):
         """Lists or host int32 arrays; k_out, v_out: device tensors, bf16 [sum n_tok][Hkv][D].  Only enqueues."""
-        lists = [np.ascontiguousarray(x, dtype=np.int32) for x in (seqs, tok_begin, n_tok)]
-        assert lists[0].size == lists[1].size == lists[2].size
-        return self.lib.kv_gather(model, lists[0].size, *[x.ctypes.data_as(C.c_void_p) for x in lists], self._p(k_out), self._p(v_out))
+        (a, pa), (b, pb), (c, pc) = _i32(seqs), _i32(tok_begin), _i32(n_tok)
+        assert a.size == b.size == c.size
+        return self.lib.kv_gather(model, a.size, pa, pb, pc, self._p(k_out), self._p(v_out))
 
     def model_set_batch(self, model, batch, row_stride):
         return self.lib.model_set_batch(model, batch, row_stride)
@@ -499,17 +505,15 @@ class PrismKV:
 
     def decode_attention_prefix_dev(self, model, q, prefix_seqs, prefix_blocks, ctx_lens, out):
         """q, ctx_lens, out: device tensors; prefix_seqs, prefix_blocks: lists or host int32 arrays, one entry a sequence.  Only enqueues."""
-        ps, pb = np.ascontiguousarray(prefix_seqs, dtype=np.int32), np.ascontiguousarray(prefix_blocks, dtype=np.int32)
+        (ps, ps_at), (pb, pb_at) = _i32(prefix_seqs), _i32(prefix_blocks)
         assert ps.size == pb.size == ctx_lens.numel()
-        return self.lib.decode_attention_prefix(model, ps.size, self._p(q), ps.ctypes.data_as(C.c_void_p), pb.ctypes.data_as(C.c_void_p),
-                                                self._p(ctx_lens), self._p(out))
+        return self.lib.decode_attention_prefix(model, ps.size, self._p(q), ps_at, pb_at, self._p(ctx_lens), self._p(out))
 
     def prefill_attention_prefix_dev(self, model, q, q_lens, prefix_seqs, prefix_blocks, ctx_lens, out):
         """The same for packed chunks; q_lens: host int32 array too.  Only enqueues."""
-        ql, ps, pb = (np.ascontiguousarray(x, dtype=np.int32) for x in (q_lens, prefix_seqs, prefix_blocks))
+        (ql, ql_at), (ps, ps_at), (pb, pb_at) = _i32(q_lens), _i32(prefix_seqs), _i32(prefix_blocks)
         assert ql.size == ps.size == pb.size == ctx_lens.numel()
-        return self.lib.prefill_attention_prefix(model, ql.size, self._p(q), ql.ctypes.data_as(C.c_void_p), ps.ctypes.data_as(C.c_void_p),
-                                                 pb.ctypes.data_as(C.c_void_p), self._p(ctx_lens), self._p(out))
+        return self.lib.prefill_attention_prefix(model, ql.size, self._p(q), ql_at, ps_at, pb_at, self._p(ctx_lens), self._p(out))
 
     def prefill_attention(self, model, q, q_lens, ctx_lens):
         """Convenience for tests: -> (code, out as numpy fp32 [sum q_lens][Hq][D])."""

@@ -693,11 +693,9 @@ static double lay_out_small(AttnGroup &grp, int size) {
 // one after the other.  Small kernel and ordinary forms, us, 32/8/128 bf16: 60 rows of 50 tokens and one of 2000 16.3, 17.2; 30 of 50 and
 // one of 4000 16.6, 20.0; 100 of 16 and one of 6000 of 8/2/128 15.5, 18.1; 120 of 39 and one of 11 055 of 8/1/128 16.9, 30.7; of 8/8/64 30 of
 // 256 and one of 4096 13.8, 20.0; 300 of 16 13.9, 13.3; 63 of 128 and one of 8192, by where the long row is, 14.6 to 20.6, 21.1.
-static bool plan_small(AttnGroup &grp) {
-    if (!g_small_now) return false;
-    int longest = 0, size = 0;
+static double best_small_part(AttnGroup &grp, int longest, int &size) {
     double best = 1e30;
-    for (int i = 0; i < grp.n; ++i) longest = longest > grp.m[i].max_pages ? longest : grp.m[i].max_pages;
+    size = 0;
     for (int part : kSmallPart) {
         const double us = lay_out_small(grp, part);
         if (us >= 0.0 && us < best) {
@@ -706,6 +704,14 @@ static bool plan_small(AttnGroup &grp) {
         }
         if (part >= longest) break;                       // longer parts change nothing
     }
+    return best;
+}
+
+static bool plan_small(AttnGroup &grp) {
+    if (!g_small_now) return false;
+    int longest = 0, size = 0;
+    for (int i = 0; i < grp.n; ++i) longest = longest > grp.m[i].max_pages ? longest : grp.m[i].max_pages;
+    const double best = best_small_part(grp, longest, size);
     if (size == 0 || best > 20.2 + 0.25e-3 * g_small_pages + longest / 136.0) return false;
     lay_out_small(grp, size);
     int begin = 0;
@@ -2198,8 +2204,15 @@ static uint64_t g_prefix_order[PKV_MAX_SEQS];
 struct PrefixCut {
     double pairs;
     int pages;
+    double us;              // what that is estimated to take beside what any such call takes
 };
 
+// Small calls take every context whole, each sequence reading its prefix for itself: one launch, and no sums through memory.  Both sides are
+// estimated; a call in two launches takes kTwoLaunchesUs more beside that.  Beyond kWholeBytes the estimate of whole contexts is too low.  Us, whole and
+// shared, of 105 random calls: 6 rows of 8/2/64 behind 320 tokens 8.6, 12.7; 44 of 5/5/128 behind three prefixes of 136 7.7, 13.2; 126 of 40/5/128
+// e4m3 behind 39 of 279 10.7, 22.0; 19 of 10/2/128 behind 2446, 1238 of their own, 17.3, 16.0; 36 of 32/8/128 behind 2925 (193 MB) 19.1, 15.7; 73 of
+// 40/5/128 behind 782 (263 MB) 29.5, 21.1.
+constexpr double kTwoLaunchesUs = 8.0, kWholeBytes = 1.0e8;
 constexpr int kMinPrefixPairs = 4;            // page pairs of a part of a prefix at least
 
 static int prefix_parts(int blocks, double part_pairs) {
@@ -2279,6 +2292,7 @@ static PrefixCut cut_prefixes(const Model &m, int batch, int tile_tok) {
     if (longest_row > cut.pages * PKV_PLAN_MAX_PARTS) cut.pages = (longest_row + PKV_PLAN_MAX_PARTS * 8 - 1) / (PKV_PLAN_MAX_PARTS * 8) * 8;
     longest = (longest + 1) / 2;
     cut.pairs = longest > 0 ? longest : 1.0;
+    cut.us = 0.0;
     const double t1 = m.dtype == PKV_BF16 ? (m.D == 128 ? 0.60 : 0.43) : (m.D == 128 ? 0.71 : 0.57), t2 = m.D == 128 ? 1.13 * t1 : 0.95 * t1;
     const double own_us = pages * (double)m.layer_bytes / 6.0e6;
     static const int kCuts[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64};
@@ -2305,7 +2319,7 @@ static PrefixCut cut_prefixes(const Model &m, int batch, int tile_tok) {
         const double rest = own_us + 0.7 * even;
         const double us = cbrt(walk * walk * walk + rest * rest * rest) + tiles * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES * (m.D + 4) * 4 * 2) / kPartBytesPerUs;
         if (us < best_us) {
-            best_us = us;
+            best_us = cut.us = us;
             cut.pairs = part;
         }
     }
@@ -2339,6 +2353,35 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
     d.cols = tile_tok * m->g;
     d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m->D));
     d.part_pages = cut.pages;
+    if (batch <= PKV_PLAN_FEW) {
+        AttnGroup grp;
+        grp.n = 1;
+        AttnDesc &w = grp.m[0];
+        w = d;
+        w.cols = m->g;
+        w.max_pages = 0;
+        g_small_rows[0] = 0;
+        SharedRows shared;
+        int64_t pages = 0;
+        for (int s = 0; s < batch; ++s) {
+            const int blocks = prefix_seqs[s] >= 0 ? prefix_blocks[s] : 0, n = m->row_len[s] + blocks;
+            shared.of[s] = SharedRow{blocks > 0 ? prefix_seqs[s] : 0, blocks};
+            w.max_pages = w.max_pages > n ? w.max_pages : n;
+            pages += n;
+        }
+        if ((double)pages * (double)m->layer_bytes < kWholeBytes) {
+            g_small_rows[0] = (int)pages;
+            int part;
+            const double us = best_small_part(grp, w.max_pages, part);
+            if (part > 0 && us < cut.us + kTwoLaunchesUs) {
+                lay_out_small(grp, part);
+                w.cnt = m->cnt;
+                w.ws = m->ws;
+                HIP_TRY(pkv_launch_prefixed_small(w, shared, g_stream));
+                return PKV_OK;
+            }
+        }
+    }
     // Plans come one after the other, sums and join, so that the next one's sums take the place of those that have been joined.
     PrefixPlan plan;
     size_t prefix_floats = 0, own_floats = 0;

@@ -342,8 +342,10 @@ struct RowPart {
 
 // JOIN: parts are joined here and rows written; wg: the work-group's number among its model's.  Otherwise the part that `at_part` says leaves its
 // sums, also where the row turns out not to have it (then maxima of -inf and denominators of 0, the others as they are).
-template <int D, int DT, bool JOIN = true>
-__device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_acc, float *s_m, float *s_l, uint32_t *s_arrived, const RowPart *at_part = nullptr) {
+// PREFIXED: a row begins with the blocks of another one, shared[seq]; nothing but logits of -inf gives zeros.
+template <int D, int DT, bool JOIN = true, bool PREFIXED = false>
+__device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_acc, float *s_m, float *s_l, uint32_t *s_arrived, const RowPart *at_part = nullptr,
+                                          const SharedRow *shared = nullptr) {
     using TL = Tile<D, DT>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int G = lane >> 4, n = lane & 15, g = d.g;
@@ -376,18 +378,45 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     // All are asked for with the context length and the queries.
     constexpr int STEP = 2 * SMALL_WAVES;
     const int ahead = STEP * (lane >> 1) + (lane & 1);
-    auto id_of = [&](int page) __attribute__((always_inline)) { return (uint32_t)row[page < d.row_stride ? page : d.row_stride - 1]; };
+    const int32_t *front = row;                           // PREFIXED: the row of its first blocks
+    int n_front = 0;
+    if constexpr (PREFIXED) {
+        n_front = __builtin_amdgcn_readfirstlane(shared[seq].blocks);
+        front = d.table + (size_t)__builtin_amdgcn_readfirstlane(shared[seq].row) * d.row_stride;
+    }
+    auto id_of = [&](int page) __attribute__((always_inline)) {
+        if constexpr (PREFIXED) {
+            const int at = page < n_front ? page : page - n_front;
+            return (uint32_t)(page < n_front ? front : row)[at < d.row_stride ? at : d.row_stride - 1];
+        }
+        return (uint32_t)row[page < d.row_stride ? page : d.row_stride - 1];
+    };
+    auto pair_ids = [&](int page) __attribute__((always_inline)) {
+        if constexpr (PREFIXED) {
+            PairIds ids;
+            ids.a = (uint32_t)__builtin_amdgcn_readfirstlane((int)id_of(page));
+            ids.b = (uint32_t)__builtin_amdgcn_readfirstlane((int)id_of(page + 1));
+            return ids;
+        }
+        return fetch_ids(d, row, page);
+    };
     int page0 = part * d.part_pages + 2 * w;
-    PairIds ids = fetch_ids(d, row, page0);
+    PairIds ids = pair_ids(page0);
     uint32_t id = id_of(page0 + STEP + ahead);
-    const int L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
+    int L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
+    if constexpr (PREFIXED) {
+        if (n_front > 0 && PKV_CONST(int32_t, d.row_len)[shared[seq].row] < n_front) {       // the prefix is not there: zero rows
+            if (threadIdx.x == 0) atomicOr(d.err, 1u);
+            L = 0;
+        } else L += n_front * T;
+    }
     const int n_pages = (L + T - 1) / T;
     int size = d.part_pages;
     if (n_pages > (JOIN ? d.parts : at_part->parts) * size) {                       // longer than the host knew
         size = (n_pages + (JOIN ? d.parts : at_part->parts) - 1) / (JOIN ? d.parts : at_part->parts);
         size = (size + STEP - 1) / STEP * STEP;
         page0 = part * size + 2 * w;
-        ids = fetch_ids(d, row, page0);
+        ids = pair_ids(page0);
         id = id_of(page0 + STEP + ahead);
     }
     const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
@@ -564,7 +593,7 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
             }
         }
         if (whole) {
-            *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + kvh * g + hn) * D + 4 * x) = n_pages > 0 ? num * (1.0f / den) : num;
+            *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + kvh * g + hn) * D + 4 * x) = n_pages > 0 && (!PREFIXED || den != 0.f) ? num * (1.0f / den) : num;
         } else {
             *reinterpret_cast<f32x4 *>(mine + hn * D + 4 * x) = num;
             if (x == 0) {
@@ -613,12 +642,12 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
 #pragma unroll
             for (int u = 0; u < 8; ++u)
                 if (c0 + u < n_parts) {
-                    const float f = __builtin_amdgcn_exp2f(s_acc[(c0 + u) * g + hn] - M);
+                    const float f = PREFIXED ? merge_weight(s_acc[(c0 + u) * g + hn], M) : __builtin_amdgcn_exp2f(s_acc[(c0 + u) * g + hn] - M);
                     den += f * s_acc[MAX_PIECES * 16 + (c0 + u) * g + hn];
                     num += f * first[u];
                 }
         }
-        *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + kvh * g + hn) * D + 4 * x) = num * (1.0f / den);
+        *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + kvh * g + hn) * D + 4 * x) = !PREFIXED || den != 0.f ? num * (1.0f / den) : num;
     }
 }
 

@@ -262,3 +262,5 @@ hipError_t pkv_launch_stream_read(const void *src, size_t bytes, size_t granule_
 hipError_t pkv_launch_prefill_prefixed(const AttnDesc &d, const ChunkPlan &plan, const SharedRows &shared, int split_groups, hipStream_t s);
 // decode behind shared prefixes: the sums of the prefixes and of the members' own rows, then the rows that they join to
 hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);
+// small calls of the same, by whole contexts; d as for a launch of the small decode kernel, at most PKV_PLAN_FEW sequences
+hipError_t pkv_launch_prefixed_small(const AttnDesc &d, const SharedRows &shared, hipStream_t s);

@@ -194,6 +194,16 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
     if (side == 0) *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + hq) * D + 4 * quad) = acc * (1.0f / den);
 }
 
+// Small calls: a work-group per part of a whole context, prefix and all, as k_attention_small; every sequence reads the prefix for itself.
+// One launch and no trip through memory where a context comes in one part.
+template <int D, int DT>
+__global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_attention_prefixed(const AttnDesc d, const SharedRows shared) {
+    __shared__ __align__(16) float s_acc[SMALL_WAVES * 16 * 128];
+    __shared__ float s_m[SMALL_WAVES * 16], s_l[SMALL_WAVES * 16];
+    __shared__ uint32_t s_arrived;
+    attn_part<D, DT, true, true>(d, (int)blockIdx.x, s_acc, s_m, s_l, &s_arrived, nullptr, shared.of);
+}
+
 template <int D, int DT, int MEET>
 void launch(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s) {
     static_assert(sizeof(AttnDesc) + sizeof(PrefixPlan) <= 4096, "a kernel's arguments end at 4 KB");
@@ -211,6 +221,18 @@ hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStrea
     } else {
         if (d.D == 128) launch<128, PKV_E4M3, 4>(d, plan, s);
         else launch<64, PKV_E4M3, 4>(d, plan, s);
+    }
+    return hipGetLastError();
+}
+
+hipError_t pkv_launch_prefixed_small(const AttnDesc &d, const SharedRows &shared, hipStream_t s) {
+    const dim3 grid((unsigned)(d.batch * d.Hkv * d.parts)), wg(64 * SMALL_WAVES);
+    if (d.dtype == PKV_BF16) {
+        if (d.D == 128) hipLaunchKernelGGL((k_attention_prefixed<128, PKV_BF16>), grid, wg, 0, s, d, shared);
+        else hipLaunchKernelGGL((k_attention_prefixed<64, PKV_BF16>), grid, wg, 0, s, d, shared);
+    } else {
+        if (d.D == 128) hipLaunchKernelGGL((k_attention_prefixed<128, PKV_E4M3>), grid, wg, 0, s, d, shared);
+        else hipLaunchKernelGGL((k_attention_prefixed<64, PKV_E4M3>), grid, wg, 0, s, d, shared);
     }
     return hipGetLastError();
 }

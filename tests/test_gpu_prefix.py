@@ -126,6 +126,25 @@ def test_infinite_logits(gpu):
     c.close()
 
 
+@pytest.mark.parametrize("hkv,blocks", [(1, 100), (8, 200)])
+def test_infinite_logits_over_many_parts(gpu, hkv, blocks):
+    """The same where contexts come in several parts: nothing but -inf gives zero rows, one row with finite keys behind them is right."""
+    d, n = 64, 12
+    own = [700] * n
+    c = P.Cache(gpu, 2 * hkv, hkv, d, BF16, own + [16 * blocks], frames=100)
+    kv = gen.seq_kv((10,), 16 * blocks, hkv, d, BF16, 16)
+    far = dict(kv, k=np.full_like(kv["k"], 0xFF80))
+    for s, x in enumerate(own + [16 * blocks]):
+        c.fill(s, kv if s == 3 else far, x)
+    q = np.full((n, 2 * hkv, d), 0x3F80, dtype=np.uint16)
+    out = torch.full((n, 2 * hkv, d), float("nan"), device="cuda")
+    assert gpu.decode_attention_prefix_dev(c.m, P.dev(q), [n] * n, [blocks] * n, P.i32(own), out) == 0
+    got = out.cpu().double().numpy()
+    want, tol = P.attention(P.f64(q[3:4]), P.f64(kv["k"][:700]), P.f64(kv["v"][:700]), [700])
+    assert np.all(np.abs(got[3:4] - want) <= tol) and (np.delete(got, 3, 0) == 0).all()
+    c.close()
+
+
 @pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
 def test_prefill(gpu, hq, hkv, d, dtype):
     """Chunks of 0, 1 and many tokens, behind tokens of their own or none, behind prefixes or none."""
@@ -265,7 +284,7 @@ def test_captured_and_replayed(gpu):
     refused = torch.cuda.CUDAGraph()
     with torch.cuda.graph(refused, stream=stream):
         gpu.use_current_stream()
-        assert calls(out, out2)[0] == -3 and "capture" in gpu.last_error()
+        assert calls(out, out2)[1] == -3 and "capture" in gpu.last_error()         # (a small decode step needs none)
     gpu.use_current_stream()
     assert calls(out, out2) == (0, 0)
     torch.cuda.synchronize()
@@ -289,6 +308,46 @@ def test_captured_and_replayed(gpu):
         if step == 2:
             big = P.dev(gen.queries((20,), 3, hq, d))
             assert gpu.decode_attention_prefix_dev(c.m, big, [4, 3, 4], [200, 40, 199], P.i32([300, 300, 300]), eager) == 0
+    assert gpu.device_errors() == 0
+    del graph, refused
+    c.close()
+
+
+def test_large_step_captured_and_replayed(gpu):
+    """The same for a decode step whose prefix is walked for all at once: refused without a workspace, then captured; a larger eager call in
+    between makes a larger workspace, and the graph goes on with its own."""
+    hq, hkv, d, n = 16, 2, 64, 60
+    rows = Rows(gpu, hq, hkv, d, BF16, [300] * n + [16 * 400, 16 * 420], frames=60)
+    c = rows.c
+    q, ctx = P.dev(gen.queries((21,), n, hq, d)), P.i32([200] * n)
+    prefix, blocks = [n] * (n - 1) + [-1], [400] * n
+    out, eager = (torch.zeros((n, hq, d), device="cuda") for _ in range(2))
+    call = lambda o, p=prefix, b=blocks: gpu.decode_attention_prefix_dev(c.m, q, p, b, ctx, o)
+    stream, graph, refused = torch.cuda.Stream(), torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(refused, stream=stream):
+        gpu.use_current_stream()
+        assert call(out) == -3 and "capture" in gpu.last_error()
+    gpu.use_current_stream()
+    assert call(out) == 0
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        gpu.use_current_stream()
+        assert call(out) == 0
+    gpu.use_current_stream()
+    for step in range(4):
+        ctx += torch.arange(n, dtype=torch.int32, device="cuda") % 7 * 3
+        q.copy_(P.dev(gen.queries((22, step), n, hq, d)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.cpu().double().numpy()
+        for s in (0, 5, n - 2, n - 1):
+            k, v = rows.context(prefix[s], blocks[s], s, int(ctx[s]))
+            want, tol = P.attention(P.f64(P.host(q)[s:s + 1]), k, v, [len(k)])
+            assert np.all(np.abs(got[s:s + 1] - want) <= tol), (step, s)
+        out.zero_()
+        if step == 1:                                                     # two groups of many parts
+            assert call(eager, [n, n + 1] * (n // 2), [400, 420] * (n // 2)) == 0
     assert gpu.device_errors() == 0
     del graph, refused
     c.close()
