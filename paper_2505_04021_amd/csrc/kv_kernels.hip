@@ -173,7 +173,9 @@ __global__ __launch_bounds__(64 * PAGE_WAVES) void k_kv_append_chunk(const AttnD
 // kv_gather: cached tokens of several sequences as packed bf16 rows, the way back of kv_append_chunk.  One wave per (sequence, page its
 // range touches, kv head, K or V): whole 16-byte units are read as they lie, 1 KiB a request, V units are transposed between the lanes
 // of a quad, and rows leave in pieces of 8 or 16 bytes, 64 side by side.  Codes are decoded, multiplied by their block's scale in fp32 and
-// rounded to bf16 once.  Bound by memory: every byte once.
+// rounded to bf16 once.  Bound by memory, every byte once, and for short ranges by its dependent trips (plan, block id, page): 8192 tokens of
+// 8/128 bf16 13.6 us (67 MB, 4.9 TB/s; a large copy 5.1); 24 ragged ranges of e4m3 caches with 64-wide heads (27 MB) 8.7, of which 5.2 for
+// the bytes (four heads a wave, all asked for at once: 9.7).
 template <int D, int DT, bool IS_V>
 __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, uint8_t *out, size_t stride, int s0, int s1) {
     const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4, G = t >> 2, e = t & 3;
