@@ -51,6 +51,11 @@ int pkv_set_kernel_form(int form);
 int pkv_last_kernel_form(void);
 /* The work items (waves; work-groups of four waves in form 2) of that launch, all its models together. */
 int pkv_last_launch_items(void);
+/* How decode_attention_prefix walks the prefixes: 0 = once for all their members, in two launches, 1 = with every context by itself, in one
+ * (where there are at most 127 sequences and the parts fit the workspace; else as 0), -1 = the library decides by the call. */
+int pkv_set_prefix_form(int form);
+/* Which of the two the most recent call took (0 or 1). */
+int pkv_last_prefix_form(void);
 /* The most parts a sequence's context came in, in the most recent prefill_attention call (1: none was cut). */
 int pkv_last_prefill_parts(void);
 /* Cost model that shares the waves out among the models of a grouped launch: a page

@@ -339,6 +339,7 @@ constexpr int kDefaultSegCost = 6;
 constexpr double kPageCost = 0.8, kDeepPageCost = 1.6;
 int g_plan_items = kDefaultItems;     // items of the launch being prepared, all models together
 AttnForm g_last_form = AttnForm::ordinary;  // what the most recent launch ran as
+int g_prefix_form = -1, g_last_prefix_form = 0;   // decode_attention_prefix: 0 prefixes once for all, 1 contexts whole, -1 by the call
 int g_last_prefill_parts = 0;         // most parts a context came in, in the most recent prefill_attention call
 int g_last_items = 0;                 // its work items, work-groups of a small launch
 bool g_small_now = false;             // the launch being prepared is a small one: a work-group per (sequence, kv head) or part of one
@@ -820,6 +821,14 @@ int pkv_last_kernel_form(void) { return g_last_form == AttnForm::small ? 2 : (g_
 int pkv_last_launch_items(void) { return g_last_items; }
 
 int pkv_last_prefill_parts(void) { return g_last_prefill_parts; }
+
+int pkv_set_prefix_form(int form) {
+    if (form < -1 || form > 1) return PKV_E_ARG;
+    g_prefix_form = form;
+    return PKV_OK;
+}
+
+int pkv_last_prefix_form(void) { return g_last_prefix_form; }
 
 int pkv_set_segment_cost(int pages) {
     if (pages < -1 || pages > 256) return PKV_E_ARG;
@@ -2215,8 +2224,9 @@ struct PrefixCut {
 constexpr double kTwoLaunchesUs = 8.0, kWholeBytes = 1.0e8;
 constexpr int kMinPrefixPairs = 4;            // page pairs of a part of a prefix at least
 
-static int prefix_parts(int blocks, double part_pairs) {
-    const int pairs = (blocks + 1) / 2, n = (int)(pairs / part_pairs + 0.999);
+// Parts of a prefix of `blocks` blocks with `columns` columns.
+static int prefix_parts(int blocks, int columns, const PrefixCut &cut) {
+    const int n = columns <= PKV_NARROW_COLUMNS ? (blocks + cut.pages - 1) / cut.pages : (int)((blocks + 1) / 2 / cut.pairs + 0.999);
     return blocks == 0 ? 0 : (n < 1 ? 1 : (n > PKV_PLAN_MAX_PARTS ? PKV_PLAN_MAX_PARTS : n));
 }
 
@@ -2224,7 +2234,7 @@ static int prefix_parts(int blocks, double part_pairs) {
 static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, int tile_tok, const PrefixCut &cut) {
     const int size = PKV_PREFILL_WAVES * tile_tok;
     p.n_groups = p.n_members = 0;
-    uint32_t unit = 0, tile = 0;
+    uint32_t units[2] = {0, 0}, tile = 0;                 // of the wide and of the narrow groups
     while (at < batch && p.n_members < PKV_PREFIX_MEMBERS && p.n_groups < PKV_PREFIX_GROUPS) {
         const uint64_t key = g_prefix_order[at] >> 16;
         auto &g = p.g[p.n_groups++];
@@ -2233,19 +2243,21 @@ static int take_prefix_plan(PrefixPlan &p, const Model &m, int batch, int at, in
             p.member[p.n_members++] = (uint16_t)(g_prefix_order[at] & 0xffff);
         const int blocks = (int)(key & 0xffffff), row = (int)(key >> 24), count = p.n_members - first;
         const int wide = (count + size - 1) / size, tiles = count < size ? (count + tile_tok - 1) / tile_tok : PKV_PREFILL_WAVES;
-        const int parts = prefix_parts(blocks, cut.pairs);
-        g.unit = unit;
+        const int parts = prefix_parts(blocks, count * m.g, cut);
+        const bool narrow = count * m.g <= PKV_NARROW_COLUMNS;
+        g.unit = units[narrow];
         g.first = (uint32_t)first | (uint32_t)(row > 0 ? row - 1 : 0) << 16;
-        g.blocks = (uint32_t)blocks | (uint32_t)parts << 24;
+        g.blocks = (uint32_t)blocks | (uint32_t)parts << 24 | (uint32_t)narrow << 31;
         g.tile = tile;
-        unit += (uint32_t)(wide * parts);
+        units[narrow] += (uint32_t)(wide * parts);
         tile += (uint32_t)(wide * parts * m.Hkv * tiles);
     }
-    p.g[p.n_groups].unit = unit;
+    p.g[p.n_groups].unit = 0;
     p.g[p.n_groups].first = (uint32_t)p.n_members;
     p.g[p.n_groups].blocks = 0;
     p.g[p.n_groups].tile = tile;
-    p.prefix_wgs = unit * (uint32_t)m.Hkv;
+    p.wide_wgs = units[0] * (uint32_t)m.Hkv;
+    p.prefix_wgs = p.wide_wgs + units[1] * (uint32_t)m.Hkv;
     // the members' own rows, longest first
     uint64_t by_length[PKV_PREFIX_MEMBERS];
     for (int i = 0; i < p.n_members; ++i) by_length[i] = (uint64_t)(uint32_t)m.row_len[p.member[i]] << 32 | (uint32_t)(PKV_PREFIX_MEMBERS - i);
@@ -2279,13 +2291,19 @@ static PrefixCut cut_prefixes(const Model &m, int batch, int tile_tok) {
     constexpr double kOwnWorkGroups = 768.0, kCUs = 256.0, kPartBytesPerUs = 3.0e6;
     const int size = PKV_PREFILL_WAVES * tile_tok;
     PrefixCut cut;
-    double pages = 0.0;
+    double pages = 0.0;                                   // of own rows and of prefixes that are walked like rows
     int longest_row = 0, longest = 0;
-    for (int s = 0; s < batch; ++s) {
-        const int blocks = (int)(g_prefix_order[s] >> 16 & 0xffffff);
-        longest = longest > blocks ? longest : blocks;
-        longest_row = longest_row > m.row_len[s] ? longest_row : m.row_len[s];
-        pages += m.row_len[s];
+    for (int i = 0, j; i < batch; i = j) {
+        for (j = i; j < batch && g_prefix_order[j] >> 16 == g_prefix_order[i] >> 16; ++j) {
+            const int row = m.row_len[g_prefix_order[j] & 0xffff];
+            longest_row = longest_row > row ? longest_row : row;
+            pages += row;
+        }
+        const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff);
+        if ((j - i) * m.g <= PKV_NARROW_COLUMNS) {
+            longest_row = longest_row > blocks ? longest_row : blocks;
+            pages += blocks;
+        } else longest = longest > blocks ? longest : blocks;
     }
     cut.pages = (int)(pages * m.Hkv / kOwnWorkGroups / 8.0 + 1.0) * 8;
     cut.pages = cut.pages < kSmallPart[0] ? kSmallPart[0] : cut.pages;
@@ -2303,8 +2321,9 @@ static PrefixCut cut_prefixes(const Model &m, int batch, int tile_tok) {
         double units = 0.0, work = 0.0, top = 0.0, tiles = 0.0;
         for (int i = 0, j; i < batch; i = j) {
             for (j = i + 1; j < batch && g_prefix_order[j] >> 16 == g_prefix_order[i] >> 16;) ++j;
-            const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff), n = prefix_parts(blocks, part);
-            if (n == 0) continue;
+            const int blocks = (int)(g_prefix_order[i] >> 16 & 0xffffff);
+            if (blocks == 0 || (j - i) * m.g <= PKV_NARROW_COLUMNS) continue;
+            const int n = prefix_parts(blocks, (j - i) * m.g, PrefixCut{part, cut.pages, 0.0});
             const double u = (double)((j - i + size - 1) / size) * n * m.Hkv, len = (double)((blocks + 1) / 2) / n;
             units += u;
             work += u * len;
@@ -2353,7 +2372,8 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
     d.cols = tile_tok * m->g;
     d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m->D));
     d.part_pages = cut.pages;
-    if (batch <= PKV_PLAN_FEW) {
+    g_last_prefix_form = 0;
+    if (batch <= PKV_PLAN_FEW && g_prefix_form != 0) {
         AttnGroup grp;
         grp.n = 1;
         AttnDesc &w = grp.m[0];
@@ -2369,14 +2389,15 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
             w.max_pages = w.max_pages > n ? w.max_pages : n;
             pages += n;
         }
-        if ((double)pages * (double)m->layer_bytes < kWholeBytes) {
+        if (g_prefix_form == 1 ? pages < INT32_MAX : (double)pages * (double)m->layer_bytes < kWholeBytes) {
             g_small_rows[0] = (int)pages;
             int part;
             const double us = best_small_part(grp, w.max_pages, part);
-            if (part > 0 && us < cut.us + kTwoLaunchesUs) {
+            if (part > 0 && (g_prefix_form == 1 || us < cut.us + kTwoLaunchesUs)) {
                 lay_out_small(grp, part);
                 w.cnt = m->cnt;
                 w.ws = m->ws;
+                g_last_prefix_form = 1;
                 HIP_TRY(pkv_launch_prefixed_small(w, shared, g_stream));
                 return PKV_OK;
             }
@@ -2387,7 +2408,7 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
     size_t prefix_floats = 0, own_floats = 0;
     auto floats = [&](size_t &prefix, size_t &own) {
         prefix = (size_t)plan.g[plan.n_groups].tile * (PKV_PREFILL_COLS / PKV_PREFILL_WAVES) * (size_t)(m->D + 4);
-        own = (size_t)plan.own_unit[PKV_PLAN_MAX_PARTS] * m->Hkv * partial_floats(m->g, m->D);
+        own = (size_t)plan.own_unit[PKV_PLAN_MAX_PARTS] * m->Hkv * m->g * (size_t)(m->D + 4);
     };
     int end = take_prefix_plan(plan, *m, batch, 0, tile_tok, cut);
     floats(prefix_floats, own_floats);

@@ -334,21 +334,37 @@ constexpr int SMALL_WAVES = 4;
 // have all waves of a part.
 __device__ __forceinline__ float merge_weight(float m, float M) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M); }
 
-// A part of a row for a kernel that joins the parts itself: which, of how many, and where its sums (partial_floats) go.
+// A part of a row for a kernel that joins the parts itself: which, of how many, of `size` pages, and where its sums go (per column D + 4
+// floats: D sums, the reference point, the denominator).  Either the row of sequence `seq` with its queries, or its first `blocks` blocks with the
+// queries of all `members`; columns: their heads, at most 16.
 struct RowPart {
-    int seq, kvh, part, parts;
+    int seq, kvh, part, parts, size, columns;
+    int blocks, first;                // -1: the sequence's own row; its first one among the launch's members
     float *sums;
 };
 
-// JOIN: parts are joined here and rows written; wg: the work-group's number among its model's.  Otherwise the part that `at_part` says leaves its
-// sums, also where the row turns out not to have it (then maxima of -inf and denominators of 0, the others as they are).
+// The queries of a part's columns as load_q has them.
+template <int D>
+__device__ __forceinline__ void load_columns(bf16x8 *qf, const AttnDesc &d, const RowPart &at, const uint16_t *members, int lane) {
+    const int G = lane >> 4, n = lane & 15, i = n / d.g;
+    const bool live = n < at.columns;
+    const int listed = (int)members[at.first + (live ? i : 0)], seq = at.blocks < 0 ? at.seq : listed;
+    const uint16_t *qrow = d.q + ((size_t)seq * d.Hq + at.kvh * d.g + n - i * d.g) * D;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        u32x4 v = mk4(0, 0, 0, 0);
+        if (live) v = *reinterpret_cast<const u32x4 *>(qrow + 8 * (4 * j + G));
+        qf[j] = *reinterpret_cast<bf16x8 *>(&v);
+    }
+}
+
 // PREFIXED: a row begins with the blocks of another one, shared[seq]; nothing but logits of -inf gives zeros.
 template <int D, int DT, bool JOIN = true, bool PREFIXED = false>
 __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_acc, float *s_m, float *s_l, uint32_t *s_arrived, const RowPart *at_part = nullptr,
-                                          const SharedRow *shared = nullptr) {
+                                          const uint16_t *members = nullptr, const SharedRow *shared = nullptr) {
     using TL = Tile<D, DT>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int G = lane >> 4, n = lane & 15, g = d.g;
+    const int G = lane >> 4, n = lane & 15, g = JOIN ? d.g : at_part->columns;
     // Work-groups are dealt to the eight XCDs in turn.  With a multiple of eight kv heads these come fastest (each XCD
     // keeps its heads), then the parts of the row, then rows: eight lognormal rows of 2048 tokens take 22 us a launch, 27
     // with the parts slowest.  Otherwise parts come slowest, so that the first parts, which every row has, fall on all
@@ -372,7 +388,8 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     const int seg = seq * d.Hkv + kvh;
     const int32_t *row = d.table + (size_t)seq * d.row_stride;
     bf16x8 qf[TL::NK];
-    load_q<D>(qf, d, seq, kvh, lane);
+    if constexpr (JOIN) load_q<D>(qf, d, seq, kvh, lane);
+    else load_columns<D>(qf, d, *at_part, members, lane);
     // This wave's pairs: pages page0 + STEP k and the one behind it, k = 0, 1, ...  The ids of the first come by themselves, those of
     // the next 32 in one read, for any row; lane i works out where page i & 1 of pair 1 + (i >> 1) is, if there is a second pair.
     // All are asked for with the context length and the queries.
@@ -400,18 +417,25 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
         }
         return fetch_ids(d, row, page);
     };
-    int page0 = part * d.part_pages + 2 * w;
+    int page0 = part * (JOIN ? d.part_pages : at_part->size) + 2 * w;
     PairIds ids = pair_ids(page0);
     uint32_t id = id_of(page0 + STEP + ahead);
-    int L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
+    int L;
+    if constexpr (JOIN) L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
+    else if (at_part->blocks < 0) L = __builtin_amdgcn_readfirstlane(ctx_clamped(d, seq));
+    else {
+        // (no branch around the length: it would not be the same for all lanes any more in the compiler's eyes)
+        const bool missing = PKV_CONST(int32_t, d.row_len)[seq] < at_part->blocks;       // the prefix is not there
+        if (missing && threadIdx.x == 0) atomicOr(d.err, 1u);
+        L = missing ? 0 : at_part->blocks * T;
+    }
     if constexpr (PREFIXED) {
-        if (n_front > 0 && PKV_CONST(int32_t, d.row_len)[shared[seq].row] < n_front) {       // the prefix is not there: zero rows
-            if (threadIdx.x == 0) atomicOr(d.err, 1u);
-            L = 0;
-        } else L += n_front * T;
+        const bool missing = n_front > 0 && PKV_CONST(int32_t, d.row_len)[shared[seq].row] < n_front;       // the prefix is not there: zero rows
+        if (missing && threadIdx.x == 0) atomicOr(d.err, 1u);
+        L = __builtin_amdgcn_readfirstlane(missing ? 0 : L + n_front * T);
     }
     const int n_pages = (L + T - 1) / T;
-    int size = d.part_pages;
+    int size = JOIN ? d.part_pages : at_part->size;
     if (n_pages > (JOIN ? d.parts : at_part->parts) * size) {                       // longer than the host knew
         size = (n_pages + (JOIN ? d.parts : at_part->parts) - 1) / (JOIN ? d.parts : at_part->parts);
         size = (size + STEP - 1) / STEP * STEP;
@@ -422,8 +446,8 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
     if (part >= n_parts) {
         if (!JOIN && (int)threadIdx.x < g) {
-            at_part->sums[g * D + threadIdx.x] = -INFINITY;
-            at_part->sums[g * D + g + threadIdx.x] = 0.f;
+            at_part->sums[threadIdx.x * (D + 4) + D] = -INFINITY;
+            at_part->sums[threadIdx.x * (D + 4) + D + 1] = 0.f;
         }
         return;
     }
@@ -595,10 +619,10 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
         if (whole) {
             *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + kvh * g + hn) * D + 4 * x) = n_pages > 0 && (!PREFIXED || den != 0.f) ? num * (1.0f / den) : num;
         } else {
-            *reinterpret_cast<f32x4 *>(mine + hn * D + 4 * x) = num;
+            *reinterpret_cast<f32x4 *>(mine + hn * (JOIN ? D : D + 4) + 4 * x) = num;
             if (x == 0) {
-                mine[g * D + hn] = M;
-                mine[g * D + g + hn] = den;
+                mine[JOIN ? g * D + hn : hn * (D + 4) + D] = M;
+                mine[JOIN ? g * D + g + hn : hn * (D + 4) + D + 1] = den;
             }
         }
     }

@@ -184,14 +184,17 @@ struct SharedRows {
 // have a k-th part are the first ones of that order and a list of counts is all there is to say.
 #define PKV_PREFIX_GROUPS 64
 #define PKV_PREFIX_MEMBERS 384
+// A group with at most so many columns (members x heads of a kv head) is walked like a row, by four waves on different pages, not by waves with 32
+// columns each on the same ones, of which one would have any.
+#define PKV_NARROW_COLUMNS 16
 struct PrefixPlan {
     int32_t n_groups, n_members;
-    uint32_t prefix_wgs;                     // work-groups for the prefixes, the launch's first
+    uint32_t wide_wgs, prefix_wgs;           // work-groups for the wide groups' prefixes, the launch's first, and with the narrow ones'
     float *own_ws;                           // sums of the own rows' parts, by unit and kv head (d.ws: those of the prefixes)
     struct {
-        uint32_t unit;                       // its first unit
+        uint32_t unit;                       // its first unit, counted among the wide or among the narrow groups'
         uint32_t first;                      // its first member | row of the prefix << 16
-        uint32_t blocks;                     // of the prefix | parts that it comes in << 24
+        uint32_t blocks;                     // of the prefix | parts that it comes in << 24 | narrow << 31
         uint32_t tile;                       // its first tile of 32 columns of d.ws
     } g[PKV_PREFIX_GROUPS + 1];              // [n_groups]: units and members in total
     uint32_t own_unit[PKV_PLAN_MAX_PARTS + 1];   // the first unit of all k-th parts; [64]: units in total, and so where there is no k-th part

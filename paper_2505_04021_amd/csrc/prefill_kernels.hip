@@ -97,11 +97,10 @@ struct PrefixedUnit : ChunkUnit {
     }
     __device__ __forceinline__ int sees(const AttnDesc &d) const {
         const int there = PKV_CONST(int32_t, d.row_len)[seq_shared], mine = ChunkUnit::sees(d);
-        if (there < blocks) {                              // (blocks <= row_stride: the host has seen to that)
-            if (threadIdx.x == 0) atomicOr(d.err, 1u);
-            return 0;
-        }
-        return PKV_T * blocks + mine;
+        // (no branch around the length: it would not be the same for all lanes any more in the compiler's eyes)
+        const bool missing = there < blocks;               // (blocks <= row_stride: the host has seen to that)
+        if (missing && threadIdx.x == 0) atomicOr(d.err, 1u);
+        return missing ? 0 : PKV_T * blocks + mine;
     }
 };
 

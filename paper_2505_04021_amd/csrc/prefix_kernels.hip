@@ -23,7 +23,7 @@ struct GroupLanes {
     }
     static __device__ __forceinline__ uint32_t of(uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)x, i); }
     __device__ __forceinline__ int first_member(const PrefixPlan &plan, int i) const {
-        return (int)((i < 64 ? of(first, i) : plan.g[64].first) & 0xffffu);
+        return (int)((i < 64 ? of(first, i) : (uint32_t)__builtin_amdgcn_readfirstlane((int)plan.g[64].first)) & 0xffffu);
     }
 };
 static_assert(PKV_PREFIX_GROUPS == 64 && PKV_PLAN_MAX_PARTS == 64, "one of each per lane");
@@ -43,38 +43,39 @@ struct PrefixUnit {
     static constexpr bool CAUSAL = false;
     // (96 rows behind 24576 tokens, without their own, in 192 work-groups 138, 146 us without levels, in 400 112.5, 115.7)
     static constexpr bool LEVELS = true;
-    const uint16_t *members;
+    const PrefixPlan &plan;
     const int32_t *shared;
-    int prefix_row, blocks, ntok, part, parts, tiles, first_tile;      // (tiles: of 32 columns, in the unit)
+    int first,                            // its first member
+        prefix_row, blocks, ntok, part, parts, tiles, first_tile;      // (tiles: of 32 columns, in the unit)
 
-    __device__ __forceinline__ PrefixUnit(const AttnDesc &d, const PrefixPlan &plan, int unit) {
+    // unit: among those of the wide or of the narrow groups
+    __device__ __forceinline__ PrefixUnit(const AttnDesc &d, const PrefixPlan &plan, int unit, bool narrow) : plan(plan) {
         const GroupLanes lanes(plan);
         const int n = plan.n_groups;
-        // groups without units share their first unit with the next one
-        const int at = __popcll(__ballot((int)(threadIdx.x & 63) < n && lanes.unit <= (uint32_t)unit)) - 1;
+        // the last of its kind that begins at or before it (groups without units share their first one with the next)
+        const int at = 63 - __clzll((long long)__ballot((int)(threadIdx.x & 63) < n && lanes.unit <= (uint32_t)unit && (lanes.blocks >> 31 != 0) == narrow));
         const uint32_t f = lanes.of(lanes.first, at), b = lanes.of(lanes.blocks, at);
-        const int first = (int)(f & 0xffffu), count = lanes.first_member(plan, at + 1) - first;
+        const int first_of_group = (int)(f & 0xffffu), count = lanes.first_member(plan, at + 1) - first_of_group;
         const GroupShape shape(d, count);
         const int u = unit - (int)lanes.of(lanes.unit, at);
         part = u / shape.wide;
         const int x = u - part * shape.wide;
-        members = plan.member + first + x * shape.size;
+        first = first_of_group + x * shape.size;
         ntok = count - x * shape.size < shape.size ? count - x * shape.size : shape.size;
         blocks = (int)(b & 0xffffffu);
-        parts = (int)(b >> 24);
+        parts = (int)(b >> 24 & 0x7fu);
         prefix_row = (int)(f >> 16);
         shared = d.table + (size_t)prefix_row * d.row_stride;
         tiles = shape.tiles;
         first_tile = (int)lanes.of(lanes.tile, at) + u * d.Hkv * tiles;
     }
     __device__ __forceinline__ uint32_t id(const AttnDesc &d, int page) const { return (uint32_t)shared[page < d.row_stride ? page : d.row_stride - 1]; }
-    __device__ __forceinline__ int row(int i) const { return members[i]; }
+    __device__ __forceinline__ int row(int i) const { return plan.member[first + i]; }
     __device__ __forceinline__ int sees(const AttnDesc &d) const {
-        if (PKV_CONST(int32_t, d.row_len)[prefix_row] < blocks) {
-            if (threadIdx.x == 0) atomicOr(d.err, 1u);
-            return 0;
-        }
-        return blocks * PKV_T;
+        // (no branch around the length: it would not be the same for all lanes any more in the compiler's eyes)
+        const bool missing = PKV_CONST(int32_t, d.row_len)[prefix_row] < blocks;
+        if (missing && threadIdx.x == 0) atomicOr(d.err, 1u);
+        return missing ? 0 : blocks * PKV_T;
     }
     __device__ __forceinline__ bool partial() const { return true; }
     __device__ __forceinline__ size_t tile(const AttnDesc &, int kvh, int w) const { return (size_t)first_tile + kvh * tiles + w; }
@@ -85,24 +86,42 @@ __global__ __launch_bounds__(64 * PF_WAVES, 2) void k_prefix_sums(const AttnDesc
     constexpr int OWN = SMALL_WAVES * 16 * D * 4 + 2 * SMALL_WAVES * 16 * 4, RING = kRingBytes<D, DT, MEET>;
     __shared__ __align__(16) uint8_t lds[OWN > RING ? OWN : RING];
     static_assert(PF_WAVES == SMALL_WAVES, "one size of work-group");
-    // Prefixes first: their walks are the longest.  (Own rows first: with the best number of cuts for either 64 rows behind 4096 tokens 42.2 and 45.8 us, 96 behind 24576 117.4 and
-    // 124.6, seven tenants on e4m3 caches 45.6 and 47.6.)
-    if (blockIdx.x < plan.prefix_wgs) {
+    // Prefixes first: their walks are the longest.  (Own rows first: with the best number of cuts for either 64 rows behind 4096 tokens 42.2
+    // and 45.8 us, 96 behind 24576 117.4 and 124.6, seven tenants on e4m3 caches 45.6 and 47.6.)
+    if (blockIdx.x < plan.wide_wgs) {
         const int unit = blockIdx.x / d.Hkv, kvh = blockIdx.x - unit * d.Hkv;
-        prefill_unit<D, DT, MEET, true>(d, PrefixUnit(d, plan, unit), kvh, lds);
+        prefill_unit<D, DT, MEET, true>(d, PrefixUnit(d, plan, unit, false), kvh, lds);
+        return;
+    }
+    RowPart at;
+    if (blockIdx.x < plan.prefix_wgs) {
+        const int x = (int)(blockIdx.x - plan.wide_wgs), unit = x / d.Hkv, kvh = x - unit * d.Hkv;
+        const PrefixUnit u(d, plan, unit, true);
+        at.seq = u.prefix_row;
+        at.kvh = kvh;
+        at.part = u.part;
+        at.parts = u.parts;
+        at.blocks = u.blocks;
+        at.size = ((u.blocks + u.parts - 1) / u.parts + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES) * (2 * SMALL_WAVES);
+        at.columns = u.ntok * d.g;
+        at.first = u.first;
+        at.sums = d.ws + u.tile(d, kvh, 0) * PF_COLS * (D + 4);
     } else {
-        float *acc = reinterpret_cast<float *>(lds), *m = acc + SMALL_WAVES * 16 * D, *l = m + SMALL_WAVES * 16;
         const int x = (int)(blockIdx.x - plan.prefix_wgs), unit = x / d.Hkv, lane = threadIdx.x & 63;
         const uint32_t from = plan.own_unit[lane], to = plan.own_unit[lane + 1];
-        RowPart at;
         at.kvh = x - unit * d.Hkv;
         at.part = __popcll(__ballot(from <= (uint32_t)unit)) - 1;
         const int rank = unit - (int)GroupLanes::of(from, at.part);
         at.parts = __popcll(__ballot(to - from > (uint32_t)rank));
         at.seq = __builtin_amdgcn_readfirstlane((int)plan.own[rank]);
-        at.sums = plan.own_ws + (size_t)x * partial_floats(d.g, D);
-        attn_part<D, DT, false>(d, 0, acc, m, l, nullptr, &at);
+        at.blocks = -1;
+        at.size = d.part_pages;
+        at.columns = d.g;
+        at.first = 0;
+        at.sums = plan.own_ws + (size_t)x * d.g * (D + 4);
     }
+    float *acc = reinterpret_cast<float *>(lds), *m = acc + SMALL_WAVES * 16 * D, *l = m + SMALL_WAVES * 16;
+    attn_part<D, DT, false>(d, 0, acc, m, l, nullptr, &at, plan.member);
 }
 
 // One wave per (member, query head): lane k holds the maximum and denominator of part k of the prefix and of the own row, then D / 4 lanes
@@ -122,7 +141,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
     const int seq = __builtin_amdgcn_readfirstlane((int)plan.member[j]), rank = __builtin_amdgcn_readfirstlane((int)plan.rank[j]);
     const int at = __popcll(__ballot(lane < plan.n_groups && (int)(lanes.first & 0xffffu) <= j)) - 1;
     const uint32_t f = lanes.of(lanes.first, at), b = lanes.of(lanes.blocks, at);
-    const int first = (int)(f & 0xffffu), blocks = (int)(b & 0xffffffu), parts = (int)(b >> 24);
+    const int first = (int)(f & 0xffffu), blocks = (int)(b & 0xffffffu), parts = (int)(b >> 24 & 0x7fu);
     const int kvh = hq / d.g, head = hq - kvh * d.g;
     const int there = PKV_CONST(int32_t, d.row_len)[f >> 16];
     // where its column is in a part of the prefix
@@ -131,21 +150,21 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
     const size_t tile0 = (size_t)lanes.of(lanes.tile, at) + (size_t)(xg * d.Hkv + kvh) * shape.tiles + w;
     const float *prefix = d.ws + (tile0 * PF_COLS + (in - w * tile_tok) * d.g + head) * (D + 4);
     const size_t prefix_step = (size_t)shape.wide * d.Hkv * shape.tiles * PF_COLS * (D + 4);
-    const int own_parts = __popcll(__ballot(to - from > (uint32_t)rank)), pf = partial_floats(d.g, D), all = parts + own_parts;
+    const int own_parts = __popcll(__ballot(to - from > (uint32_t)rank)), all = parts + own_parts;
     auto own_part = [&](uint32_t k_from) __attribute__((always_inline)) {
-        return plan.own_ws + ((size_t)(k_from + (uint32_t)rank) * d.Hkv + kvh) * pf;
+        return plan.own_ws + (((size_t)(k_from + (uint32_t)rank) * d.Hkv + kvh) * d.g + head) * (D + 4);
     };
 
     float m[2], l[2];
     {
-        const float *p = prefix + (lane < parts ? lane : 0) * prefix_step + D, *o = own_part(lane < own_parts ? from : lanes.of(from, 0)) + d.g * D + head;
+        const float *p = prefix + (lane < parts ? lane : 0) * prefix_step + D, *o = own_part(lane < own_parts ? from : lanes.of(from, 0)) + D;
         m[0] = l[0] = 0.f;
         if (parts > 0) {
             m[0] = p[0];
             l[0] = p[1];
         }
         m[1] = o[0];
-        l[1] = o[d.g];
+        l[1] = o[1];
     }
     const int quad = lane % QUADS, side = lane / QUADS;
     f32x4 v[TRIP];
@@ -155,7 +174,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
             int p = p0 + SIDE * k + side;
             p = p < all ? p : all - 1;
             const uint32_t k_from = (uint32_t)__shfl((int)from, p < parts ? 0 : p - parts);
-            const float *src = p < parts ? prefix + p * prefix_step : own_part(k_from) + head * D;
+            const float *src = p < parts ? prefix + p * prefix_step : own_part(k_from);
             v[k] = *reinterpret_cast<const f32x4 *>(src + 4 * quad);
         }
     };
@@ -201,7 +220,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_attention_prefixed(cons
     __shared__ __align__(16) float s_acc[SMALL_WAVES * 16 * 128];
     __shared__ float s_m[SMALL_WAVES * 16], s_l[SMALL_WAVES * 16];
     __shared__ uint32_t s_arrived;
-    attn_part<D, DT, true, true>(d, (int)blockIdx.x, s_acc, s_m, s_l, &s_arrived, nullptr, shared.of);
+    attn_part<D, DT, true, true>(d, (int)blockIdx.x, s_acc, s_m, s_l, &s_arrived, nullptr, nullptr, shared.of);
 }
 
 template <int D, int DT, int MEET>

@@ -19,6 +19,14 @@ def gpu():
     return PrismKV()
 
 
+@pytest.fixture(params=[0, 1], ids=["once for all", "whole contexts"])
+def form(gpu, request):
+    """Both ways of walking the prefixes of a decode step."""
+    assert gpu.set_prefix_form(request.param) == 0
+    yield request.param
+    gpu.set_prefix_form(-1)
+
+
 def values(kv, dtype):
     """K and V of gen.seq_kv as float64."""
     if dtype == BF16:
@@ -56,7 +64,7 @@ def check_decode(gpu, rows, q, prefix, blocks, ctx):
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
-def test_decode(gpu, hq, hkv, d, dtype):
+def test_decode(gpu, form, hq, hkv, d, dtype):
     """Groups of 1 to many members in no order, prefixes of one block to many and odd numbers, rows with and without a prefix, without tokens
     of their own, without either; the same row shared to different depths; a row of the batch that is itself a prefix."""
     n = 45
@@ -79,6 +87,24 @@ def test_decode(gpu, hq, hkv, d, dtype):
     rows.c.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 2, 128, BF16), (6, 2, 64, E4M3), (5, 5, 64, BF16), (16, 1, 128, E4M3)])
+def test_decode_narrow_groups(gpu, form, hq, hkv, d, dtype):
+    """Groups of few columns (members x heads of a kv head: up to 16, one more, many), whose prefixes are walked by four waves on different
+    pages, between groups whose prefixes are not and sequences without one; prefixes of one block, of odd numbers and of many parts."""
+    g = hq // hkv
+    sizes = [1, 16 // g, 16 // g + 1, 2, 40, 1]
+    shared = [16, 16 * 7, 16 * 90, 16 * 300, 16 * 33, 16 * 131]
+    group = [j for j, n in enumerate(sizes) for _ in range(n)] + [-1] * 3
+    group = [group[i] for i in np.random.default_rng(g).permutation(len(group))]
+    n = len(group)
+    own = [int(x) for x in gen.ctx_lognormal(n, 30, 1.2, 300, gen.generator(23, hq))]
+    own[0] = 0
+    rows = Rows(gpu, hq, hkv, d, dtype, own + shared, frames=100)
+    check_decode(gpu, rows, gen.queries((24, d), n, hq, d), [n + x if x >= 0 else -1 for x in group], [shared[x] // 16 if x >= 0 else 0 for x in group], own)
+    assert gpu.last_prefix_form() == form and gpu.device_errors() == 0
+    rows.c.close()
+
+
 def test_decode_many_groups_and_members(gpu):
     """More groups, and more members of one, than a launch's plan holds."""
     hq, hkv, d, n = 4, 1, 64, 1300
@@ -95,7 +121,7 @@ def test_decode_many_groups_and_members(gpu):
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(16, 2, 128, BF16), (8, 8, 64, E4M3)])
-def test_decode_long_rows(gpu, hq, hkv, d, dtype):
+def test_decode_long_rows(gpu, form, hq, hkv, d, dtype):
     """Long prefixes and long rows, both in many parts; one long row among short ones."""
     own = [5000, 3, 700, 2900]
     rows = Rows(gpu, hq, hkv, d, dtype, own + [16 * 401], frames=100)
@@ -106,7 +132,7 @@ def test_decode_long_rows(gpu, hq, hkv, d, dtype):
     rows.c.close()
 
 
-def test_infinite_logits(gpu):
+def test_infinite_logits(gpu, form):
     """Keys of -inf against positive queries weigh nothing, wherever they stand: all of a prefix, all of a row, or both (then the row is zero)."""
     hq, hkv, d = 4, 2, 64
     c = P.Cache(gpu, hq, hkv, d, BF16, [40, 40, 40, 64, 64], frames=4)
@@ -127,7 +153,7 @@ def test_infinite_logits(gpu):
 
 
 @pytest.mark.parametrize("hkv,blocks", [(1, 100), (8, 200)])
-def test_infinite_logits_over_many_parts(gpu, hkv, blocks):
+def test_infinite_logits_over_many_parts(gpu, form, hkv, blocks):
     """The same where contexts come in several parts: nothing but -inf gives zero rows, one row with finite keys behind them is right."""
     d, n = 64, 12
     own = [700] * n
@@ -225,6 +251,7 @@ def test_refusals(gpu):
         assert f([2, 2], [2, 2], q=q.view(-1)[1:]) == -1 and f([2, 2], [2, 2], o=out.view(-1)[1:]) == -1
         assert f([2, 2], [2, 2], o=None) == -1
         assert f([-1, -1], [99, 0]) == 0                                  # no prefix: its blocks are not looked at
+    assert gpu.set_prefix_form(2) == -1 and gpu.set_prefix_form(-2) == -1
     four = P.i32([1, 1, 1, 1])
     assert gpu.decode_attention_prefix_dev(c.m, q, [2] * 4, [1] * 4, four, out) == -6
     assert pre([2, 2], [2, 2], ql=(1, -1)) == -1 and pre([2, 2], [2, 2], ql=(1 << 24, 1)) == -6 and pre([2, 2], [2, 2], ql=(0, 0)) == 0
@@ -247,8 +274,9 @@ def test_prefix_that_is_not_there(gpu):
     ticket = gpu.seq_reserve_batch_enqueue(m, [2], [16 * 500])
     assert ticket >= 0
     q = gen.queries((17,), 2, 8, 64)
-    for prefill in (False, True):
+    for prefill, how in ((False, 0), (False, 1), (True, -1)):
         out = torch.full((2, 8, 64), float("nan"), device="cuda")
+        assert gpu.set_prefix_form(how) == 0
         if prefill:
             rc = gpu.prefill_attention_prefix_dev(m, P.dev(q), [1, 1], [2, -1], [400, 0], P.i32([20, 20]), out)
         else:
@@ -257,6 +285,7 @@ def test_prefix_that_is_not_there(gpu):
         got = out.cpu().double().numpy()
         want, tol = P.attention(P.f64(q[1:]), P.f64(kv["k"]), P.f64(kv["v"]), [20])
         assert (got[0] == 0).all() and np.all(np.abs(got[1:] - want) <= tol)
+    gpu.set_prefix_form(-1)
     assert gpu.device_errors() == 5 and gpu.ticket_result(ticket) == -4
     assert gpu.decode_attention_prefix_dev(m, P.dev(q), [2, -1], [400, 0], P.i32([20, 20]), out) == -6      # now the host knows
     for s in range(3):

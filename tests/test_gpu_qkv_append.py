@@ -206,6 +206,8 @@ def test_refusals(gpu):
     assert gpu.qkv_append_dev(c.m, q, k, v, P.i32([1, 1, 1]), out) == -6                       # more rows than the model has
     assert gpu.qkv_append_dev(c.m, q, k, v, one, None) == -1
     assert gpu.qkv_append_dev(c.m, q, k, v, one, out.view(-1)[1:], **ok) == -1    # q_out not on 16 bytes
+    odd = torch.ones(d + 8, dtype=torch.bfloat16, device="cuda")[1:1 + d]
+    assert gpu.qkv_append_dev(c.m, q, k, v, one, out, q_weight=odd) == -1 and gpu.qkv_append_dev(c.m, q, k, v, one, out, k_weight=odd) == -1
     assert gpu.qkv_append_dev(c.m, q, k, v, one, out, eps=-1.0, **ok) == -1
     assert gpu.qkv_append_dev(c.m, q, k, v, one, out, eps=float("nan"), **ok) == -1
     assert gpu.qkv_append_dev(c.m, q, k, v, one, out, rotary=5) == -2 and gpu.qkv_append_dev(c.m, q, k, v, one, out, rotary=-2) == -2
