@@ -398,7 +398,8 @@ int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens
  * with the same prefix_seqs and prefix_blocks form a group; a group's prefix is read once for all its members,
  * in any order of the batch.
  * prefill_attention_prefix: query i of sequence s stands behind the prefix and ctx_lens[s] - q_lens[s] + i
- * tokens of its own and sees all of those and itself. */
+ * tokens of its own and sees all of those and itself; one that would stand before its row's first token
+ * (ctx_lens[s] below q_lens[s]) sees the prefix alone, as a decode step with a context length of 0 does. */
 int decode_attention_prefix(int model, int batch, const void *q, const int32_t *prefix_seqs,
                             const int32_t *prefix_blocks, const int32_t *ctx_lens, float *out);
 int prefill_attention_prefix(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *prefix_seqs,

@@ -51,7 +51,8 @@ __device__ __forceinline__ GroupInfo group_info(const AttnDesc &d, const PlanOf<
 
 // A group of a chunk's query tokens in front of its own row.
 struct ChunkUnit {
-    static constexpr bool CAUSAL = true, LEVELS = true;
+    static constexpr bool CAUSAL = true, LEVELS = true, SHARED = false;
+    __device__ __forceinline__ int front() const { return 0; }
     int seq, q0, ntok, back, part, parts, slot;
     const int32_t *own;
     __device__ __forceinline__ ChunkUnit(const GroupInfo &g, const AttnDesc &d, int group)
@@ -87,6 +88,8 @@ __global__ __launch_bounds__(64 * PF_WAVES, 2) void k_prefill(const AttnDesc d, 
 // Chunks of sequences that share a prefix: the blocks of the prefix's row, then the sequence's own, as one context.  Whole blocks are
 // shared, so the walk need not know where the one ends and the other begins.  Probabilities keep 16 bits on both cache types.
 struct PrefixedUnit : ChunkUnit {
+    static constexpr bool SHARED = true;
+    __device__ __forceinline__ int front() const { return PKV_T * blocks; }
     const int32_t *shared;
     int seq_shared, blocks;
     __device__ __forceinline__ PrefixedUnit(const GroupInfo &g, const AttnDesc &d, int group, const SharedRow &p)

@@ -70,6 +70,7 @@ constexpr int kRingBytes = 2 * (2 * MEET) * 2 * PfTile<D, DT>::BYTES;
 //   row(i)                     packed row of q (and out) of query token i
 //   sees(d)                    tokens that the last query sees, never beyond what the rows hold
 //   partial()                  whether sums go to d.ws for a later join, or rows to out
+//   SHARED, front()            whether contexts begin with tokens of another row, and how many: every query sees at least those
 //   CAUSAL                     token i sees ntok - 1 - i tokens fewer than the last one; otherwise all see the same
 // LOW: probabilities reach the matrix unit with 16 significant bits (bf16 high and low halves), else with 8.
 template <int D, int DT, int MEET, bool LOW, typename UNIT>
@@ -112,11 +113,13 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     const int p_end = p_begin + per < n_pairs ? p_begin + per : n_pairs;
     const int np = p_end - p_begin;
     // pairs below it hold only tokens that every column sees
-    const int causal_from = UNIT::CAUSAL ? L - (ntok - 1) : L;
+    const int least = UNIT::SHARED ? (u.front() < L ? u.front() : L) : 0;
+    auto at_least = [&](int sees) __attribute__((always_inline)) { return UNIT::SHARED && sees < least ? least : sees; };
+    const int causal_from = at_least(UNIT::CAUSAL ? L - (ntok - 1) : L);
     const int p_plain = causal_from > 0 ? causal_from >> 5 : 0;
 
-    const int col_lim = UNIT::CAUSAL && col_live ? L - (ntok - 1 - (t0 + tok)) : L;                  // tokens this column sees
-    const int tile_lim = my_tok > 0 ? L - (UNIT::CAUSAL ? ntok - t0 - my_tok : 0) : 0;               // tokens some column of the tile sees
+    const int col_lim = at_least(UNIT::CAUSAL && col_live ? L - (ntok - 1 - (t0 + tok)) : L);        // tokens this column sees
+    const int tile_lim = my_tok > 0 ? at_least(L - (UNIT::CAUSAL ? ntok - t0 - my_tok : 0)) : 0;     // tokens some column of the tile sees
 
     f32x16 acc[TL::ND];
 #pragma unroll

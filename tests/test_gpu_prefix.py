@@ -215,6 +215,27 @@ def test_prefill_few_queries_behind_a_long_prefix(gpu, hq, hkv, d, dtype):
     rows.c.close()
 
 
+@pytest.mark.parametrize("d,dtype", [(128, BF16), (64, E4M3)])
+def test_prefill_of_queries_before_their_row(gpu, d, dtype):
+    """Context lengths below the chunk's: queries that would stand before their row's first token see the prefix alone."""
+    hq, hkv = 8, 2
+    have, new, ctx = [100, 60, 40, 10], [90, 60, 40, 10], [70, 13, 0, -5]
+    rows = Rows(gpu, hq, hkv, d, dtype, have + [16 * 20], frames=20)
+    q = gen.queries((25, d), sum(new), hq, d)
+    for blocks in (20, 1, 0):
+        out = torch.full((sum(new), hq, d), float("nan"), device="cuda")
+        assert gpu.prefill_attention_prefix_dev(rows.c.m, P.dev(q), new, [4] * 4, [blocks] * 4, P.i32(ctx), out) == 0
+        got, at = out.cpu().double().numpy(), 0
+        for s in range(4):
+            k, v = rows.context(4, blocks, s, max(ctx[s], 0))
+            own = [ctx[s] - new[s] + 1 + i for i in range(new[s])]
+            want, tol = P.attention(P.f64(q[at:at + new[s]]), k, v, [16 * blocks + max(x, 0) for x in own])
+            assert np.all(np.abs(got[at:at + new[s]] - want) <= tol), (blocks, s)
+            at += new[s]
+    assert gpu.device_errors() == 0
+    rows.c.close()
+
+
 def test_prefill_of_many_sequences(gpu):
     """More sequences than a launch of this kind holds."""
     hq, hkv, d, n = 4, 1, 64, 300
