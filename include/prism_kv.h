@@ -85,8 +85,8 @@ int pkv_set_stream(void *hip_stream);
 /* Text of the last HIP / library error on this thread (never NULL). */
 const char *pkv_last_error(void);
 /* Sticky device-side error flags raised by calls that only enqueue (bit 0: a block id outside
- * the pool was met in decode_attention, that page was skipped; bit 1: kv_append met a context
- * length outside the row's blocks; bit 2: an enqueue-only bookkeeping call was refused).
+ * the pool was met by an attention call or a kv_gather, that page was skipped, or a shared prefix was not there;
+ * bit 1: kv_append or qkv_append met a context length outside the row's blocks; bit 2: an enqueue-only bookkeeping call was refused).
  * Synchronises the stream; clears the flags. */
 int pkv_device_errors(void);
 

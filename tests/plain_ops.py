@@ -77,12 +77,16 @@ def attention(q, k, v, limits):
 
 class Cache:
     """One model on the library whose rows hold `lens` tokens of room; blocks of the rows interleave over scattered frames, and every byte
-    of the pool is a NaN until it is written."""
+    of the pool is a NaN until it is written (not of an elastic one)."""
 
-    def __init__(self, be, hq, hkv, d, dtype, lens, seed=3, frames=48, frame_bytes=1 << 20, poison=0xFF, n_layers=1):
+    def __init__(self, be, hq, hkv, d, dtype, lens, seed=3, frames=48, frame_bytes=1 << 20, poison=0xFF, n_layers=1, elastic=False):
         self.be, self.hq, self.hkv, self.d, self.dtype, self.lens = be, hq, hkv, d, dtype, list(lens)
-        self.storage = torch.full((frames * frame_bytes,), poison, dtype=torch.uint8, device="cuda")
-        self.pool = be.pool_create(frames * frame_bytes, T, frame_bytes, self.storage)
+        if elastic:
+            frame_bytes = 2 << 20
+            self.pool = be.pool_create_elastic(frames * frame_bytes, T, frame_bytes)
+        else:
+            self.storage = torch.full((frames * frame_bytes,), poison, dtype=torch.uint8, device="cuda")
+            self.pool = be.pool_create(frames * frame_bytes, T, frame_bytes, self.storage)
         assert self.pool >= 0 and be.pool_seed_free_order(self.pool, gen.free_order(frames, gen.generator(seed, 1))) == 0
         self.m = be.model_register(self.pool, hq, hkv, d, dtype, len(lens), max(1, max(-(-n // T) for n in lens)), n_layers)
         assert self.m >= 0 and be.balloon_resize(self.m, frames) == frames

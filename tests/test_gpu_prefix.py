@@ -465,3 +465,55 @@ def test_from_system_prompt_to_answers(gpu, dtype):
     assert gpu.device_errors() == 0
     gpu.rotary_destroy(rid)
     c.close()
+
+
+def test_layers_of_two_models_on_two_streams(gpu):
+    """Models of several layers in elastic pools, each on a stream of its own, their calls in turn: a prefix and prompts behind it appended and
+    attended to, then a decode step, layer by layer; all of it looked at when everything has been enqueued.  (Prompts end with a block: appended behind
+    them, a decode step's token rescales no codes that the prompts' queries saw.)"""
+    models = [(8, 2, 128, BF16, 3), (12, 4, 64, E4M3, 2)]
+    new, prefix, blocks = [32, 64, 16, 16 * 12], [3, 3, -1, -1], [12, 7, 0, 0]
+    n, todo = sum(new[:3]), []
+    caches = [P.Cache(gpu, hq, hkv, d, t, [x + 1 for x in new], frames=4, n_layers=layers, elastic=True) for hq, hkv, d, t, layers in models]
+    streams = [torch.cuda.Stream() for _ in models]
+    rids = [gpu.rotary_create(m[2], i, P.frequencies(m[2])) for i, m in enumerate(models)]
+    before, lens, now, dec = P.i32([16 * b for b in blocks]), P.i32(new), P.i32(new[:3]), P.i32([x + 1 for x in new[:3]])
+    data = {}
+    for i, (hq, hkv, d, _, layers) in enumerate(models):
+        for layer in range(layers):
+            for key, rows in ((0, sum(new)), (1, 3)):
+                x = P.dev(gen.randn_bf16((rows, (hq + 2 * hkv) * d), gen.generator(50, i, layer, key))).view(rows, -1, d)
+                data[i, layer, key] = (x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], torch.empty((rows, hq, d), dtype=torch.int16, device="cuda"))
+            data[i, layer, 2] = [torch.full((rows, hq, d), float("nan"), device="cuda") for rows in (n, 3)]
+    torch.cuda.synchronize()
+    for layer in range(3):
+        for i, (c, m) in enumerate(zip(caches, models)):
+            if layer >= m[4]:
+                continue
+            with torch.cuda.stream(streams[i]):
+                gpu.use_current_stream()
+                assert gpu.set_layer(c.m, layer) == 0
+                (q, k, v, qo), (q1, k1, v1, qo1), out = (data[i, layer, key] for key in range(3))
+                assert gpu.qkv_append_chunk_dev(c.m, q, k, v, new, lens, qo, None, None, 0.0, rids[i], before) == sum(new)
+                assert gpu.prefill_attention_prefix_dev(c.m, qo, new[:3], prefix[:3], blocks[:3], now, out[0]) == 0
+                assert gpu.qkv_append_dev(c.m, q1, k1, v1, dec, qo1, None, None, 0.0, rids[i], before) == 3
+                assert gpu.decode_attention_prefix_dev(c.m, qo1, prefix[:3], blocks[:3], dec, out[1]) == 0
+                todo.append((i, layer))
+    torch.cuda.synchronize()
+    gpu.use_current_stream()
+    for i, layer in todo:
+        c = caches[i]
+        gpu.set_layer(c.m, layer)
+        front, at = c.read(3, 0, 16 * 12), 0
+        for s in range(3):
+            k, v = (np.concatenate([a[:16 * blocks[s]], b]) for a, b in zip(front, c.read(s, 0, new[s] + 1)))
+            for q, out, rows, seen in ((data[i, layer, 0][3], data[i, layer, 2][0], slice(at, at + new[s]), [16 * blocks[s] + 1 + j for j in range(new[s])]),
+                                       (data[i, layer, 1][3], data[i, layer, 2][1], slice(s, s + 1), [len(k)])):
+                want, tol = P.attention(P.f64(P.host(q)[rows]), k, v, seen)
+                assert np.all(np.abs(out[rows].cpu().double().numpy() - want) <= tol), (i, layer, s, len(seen))
+            at += new[s]
+    assert gpu.device_errors() == 0
+    for rid in rids:
+        gpu.rotary_destroy(rid)
+    for c in caches:
+        c.close()
