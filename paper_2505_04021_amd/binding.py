@@ -6,6 +6,7 @@ numpy inputs are copied to the device first.  No step of the path runs in Python
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -14,11 +15,8 @@ ROTARY_HALF, ROTARY_PAIRS = 0, 1
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 
 
-class _Qkv(C.Structure):
-    """pkv_qkv"""
-    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
-                ("v_stride", C.c_int64), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rotary", C.c_int),
-                ("before", C.c_void_p)]
+# pkv_qkv: q, k, v, their strides, q_weight, k_weight, eps, rotary, before
+_QKV = struct.Struct("@PPPqqqPPfiP")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -122,10 +120,15 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
            "kv_gather", "decode_attention_prefix", "prefill_attention_prefix"]
 
 
+# Calls of few tokens take the host longer than the GPU: their addresses go as plain integers and their host lists as bytes, not as c_void_p and numpy
+# arrays' addresses (qkv_append 4.8 us without the library's part before, decode_attention_prefix 4.7, kv_gather 6.0; 4.0, 1.9 and 2.4 so).
+def _at(tensor):
+    return None if tensor is None else tensor.data_ptr()
+
+
 def _i32(a):
-    """(array, address) of a host int32 list; the array has to outlive the call."""
-    a = np.ascontiguousarray(a, dtype=np.int32)
-    return a, a.__array_interface__["data"][0]
+    """A host int32 list or array as the bytes that a call reads."""
+    return np.asarray(a, dtype=np.int32).tobytes()
 
 
 def _f64(a):
@@ -183,7 +186,6 @@ class PrismKV:
         self.lib = _load()
         self._shape = {}
         self._keep = {}
-        self._qkv_args = _Qkv()                    # (the call reads it before it returns)
         self.use_current_stream()
 
     # ---- host policies (no GPU work)
@@ -418,34 +420,29 @@ class PrismKV:
     def rotary_destroy(self, rotary):
         return self.lib.rotary_destroy(rotary)
 
+    @staticmethod
+    def _rows(x, heads, d):
+        """Address and distance of tokens whose heads lie side by side."""
+        n, h, e = x.shape
+        token, head, one = x.stride()
+        assert h == heads and e == d and one == 1 and (head == d or h == 1) and x.element_size() == 2
+        return x.data_ptr(), token if n > 1 else 0
+
     def _qkv(self, model, q, k, v, q_weight, k_weight, eps, rotary, before):
         hq, hkv, d, _ = self._shape[model]
-        args = self._qkv_args
-        strides = []
-        for x, heads in ((q, hq), (k, hkv), (v, hkv)):
-            # a token's heads side by side, tokens any distance apart
-            shape, stride = x.shape, x.stride()
-            assert len(shape) == 3 and shape[1] == heads and shape[2] == d and x.element_size() == 2
-            assert stride[2] == 1 and (heads == 1 or stride[1] == d)
-            strides.append(stride[0] if shape[0] > 1 else 0)
-        args.q, args.k, args.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-        args.q_stride, args.k_stride, args.v_stride = strides
-        args.q_weight = None if q_weight is None else q_weight.data_ptr()
-        args.k_weight = None if k_weight is None else k_weight.data_ptr()
-        args.before = None if before is None else before.data_ptr()
-        args.eps, args.rotary = eps, rotary
-        return C.byref(args)
+        (q, qs), (k, ks), (v, vs) = self._rows(q, hq, d), self._rows(k, hkv, d), self._rows(v, hkv, d)
+        return _QKV.pack(q, k, v, qs, ks, vs, _at(q_weight) or 0, _at(k_weight) or 0, eps, rotary, _at(before) or 0)
 
     def qkv_append_dev(self, model, q, k, v, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues."""
         x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append(model, ctx_lens.numel(), x, self._p(ctx_lens), self._p(q_out))
+        return self.lib.qkv_append(model, ctx_lens.numel(), x, _at(ctx_lens), _at(q_out))
 
     def qkv_append_chunk_dev(self, model, q, k, v, q_lens, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
-        """The same for packed chunks; q_lens: host int32 numpy array.  Only enqueues."""
-        ql, ql_at = _i32(q_lens)
+        """The same for packed chunks; q_lens: list or host int32 array.  Only enqueues."""
+        ql = _i32(q_lens)
         x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append_chunk(model, ql.size, x, ql_at, self._p(ctx_lens), self._p(q_out))
+        return self.lib.qkv_append_chunk(model, len(ql) // 4, x, ql, _at(ctx_lens), _at(q_out))
 
     def kv_read(self, model, seq, tok_begin, n_tok):
         """-> (code, k, v, k_scale, v_scale) as numpy: elements [n_tok][Hkv][D], scales [n_tok][Hkv] (None for bf16)."""
@@ -467,9 +464,9 @@ class PrismKV:
 
     def kv_gather_dev(self, model, seqs, tok_begin, n_tok, k_out, v_out):
         """Lists or host int32 arrays; k_out, v_out: device tensors, bf16 [sum n_tok][Hkv][D].  Only enqueues."""
-        (a, pa), (b, pb), (c, pc) = _i32(seqs), _i32(tok_begin), _i32(n_tok)
-        assert a.size == b.size == c.size
-        return self.lib.kv_gather(model, a.size, pa, pb, pc, self._p(k_out), self._p(v_out))
+        a, b, c = _i32(seqs), _i32(tok_begin), _i32(n_tok)
+        assert len(a) == len(b) == len(c)
+        return self.lib.kv_gather(model, len(a) // 4, a, b, c, _at(k_out), _at(v_out))
 
     def model_set_batch(self, model, batch, row_stride):
         return self.lib.model_set_batch(model, batch, row_stride)
@@ -513,15 +510,15 @@ class PrismKV:
 
     def decode_attention_prefix_dev(self, model, q, prefix_seqs, prefix_blocks, ctx_lens, out):
         """q, ctx_lens, out: device tensors; prefix_seqs, prefix_blocks: lists or host int32 arrays, one entry a sequence.  Only enqueues."""
-        (ps, ps_at), (pb, pb_at) = _i32(prefix_seqs), _i32(prefix_blocks)
-        assert ps.size == pb.size == ctx_lens.numel()
-        return self.lib.decode_attention_prefix(model, ps.size, self._p(q), ps_at, pb_at, self._p(ctx_lens), self._p(out))
+        ps, pb, n = _i32(prefix_seqs), _i32(prefix_blocks), ctx_lens.numel()
+        assert len(ps) == len(pb) == 4 * n
+        return self.lib.decode_attention_prefix(model, n, _at(q), ps, pb, _at(ctx_lens), _at(out))
 
     def prefill_attention_prefix_dev(self, model, q, q_lens, prefix_seqs, prefix_blocks, ctx_lens, out):
         """The same for packed chunks; q_lens: host int32 array too.  Only enqueues."""
-        (ql, ql_at), (ps, ps_at), (pb, pb_at) = _i32(q_lens), _i32(prefix_seqs), _i32(prefix_blocks)
-        assert ql.size == ps.size == pb.size == ctx_lens.numel()
-        return self.lib.prefill_attention_prefix(model, ql.size, self._p(q), ql_at, ps_at, pb_at, self._p(ctx_lens), self._p(out))
+        ql, ps, pb, n = _i32(q_lens), _i32(prefix_seqs), _i32(prefix_blocks), ctx_lens.numel()
+        assert len(ql) == len(ps) == len(pb) == 4 * n
+        return self.lib.prefill_attention_prefix(model, n, _at(q), ql, ps, pb, _at(ctx_lens), _at(out))
 
     def prefill_attention(self, model, q, q_lens, ctx_lens):
         """Convenience for tests: -> (code, out as numpy fp32 [sum q_lens][Hq][D])."""
