@@ -86,7 +86,8 @@ __global__ __launch_bounds__(64 * PF_WAVES, 2) void k_prefill(const AttnDesc d, 
 }
 
 // Chunks of sequences that share a prefix: the blocks of the prefix's row, then the sequence's own, as one context.  Whole blocks are
-// shared, so the walk need not know where the one ends and the other begins.  Probabilities keep 16 bits on both cache types.
+// shared, so the walk need not know where the one ends and the other begins.  Probabilities keep 16 bits on both cache types,
+// so that a token's output does not depend on whether it came in a chunk or in a decode step (2.5e-6 from 64 bits either way).
 struct PrefixedUnit : ChunkUnit {
     static constexpr bool SHARED = true;
     __device__ __forceinline__ int front() const { return PKV_T * blocks; }
