@@ -178,7 +178,7 @@ __global__ __launch_bounds__(64 * PAGE_WAVES) void k_kv_append_chunk(const AttnD
 // the bytes (four heads a wave, all asked for at once: 9.7).
 template <int D, int DT, bool IS_V>
 __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, uint8_t *out, size_t stride, int s0, int s1) {
-    const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4, G = t >> 2, e = t & 3;
+    const int lane = threadIdx.x & 63, t = IS_V ? lane & 15 : lane >> 2, c = IS_V ? lane >> 4 : lane & 3, G = t >> 2, e = t & 3;
     constexpr int N = DT == PKV_BF16 ? D / 32 : D / 64;
     u32x4 u[N];
     const u32x4 *unit = reinterpret_cast<const u32x4 *>(tile + (IS_V ? (G * 16 + 4 * c + e) * 16 : (c * 16 + t) * 16));
@@ -186,26 +186,30 @@ __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, ui
     for (int i = 0; i < N; ++i) u[i] = unit[64 * i];
     const bool mine = t >= s0 && t < s1;
     uint8_t *row = out + (ptrdiff_t)(t - s0) * (ptrdiff_t)stride;
-    auto put4 = [&](int at, u32x2 w) __attribute__((always_inline)) { if (mine) *reinterpret_cast<u32x2 *>(row + 2 * at) = w; };
     auto values = [&](uint32_t codes) __attribute__((always_inline)) {
         const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
         return mk2(pack_bf16_rne(a[0] * scale, a[1] * scale), pack_bf16_rne(b[0] * scale, b[1] * scale));
     };
     auto put8 = [&](int at, u32x4 w) __attribute__((always_inline)) { if (mine) *reinterpret_cast<u32x4 *>(row + 2 * at) = w; };
+    // elements at + 4 c .. + 3 (lo) and at + 16 + 4 c .. + 3 (hi): lanes c and c ^ 1 exchange, so that either has eight in a row
+    auto put_pair = [&](int at, u32x2 lo, u32x2 hi) __attribute__((always_inline)) {
+        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+        const u2 a = __builtin_amdgcn_permlane16_swap(lo.x, hi.x, false, false), b = __builtin_amdgcn_permlane16_swap(lo.y, hi.y, false, false);
+        put8(at + 16 * (c & 1) + 8 * (c >> 1), mk4(a.x, b.x, a.y, b.y));
+    };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if constexpr (DT == PKV_BF16 && !IS_V) {
             put8(8 * (4 * i + c), u[i]);
         } else if constexpr (DT == PKV_BF16) {
-            put4(32 * i + 4 * c, transpose_halves(u[i].x, u[i].y, e));
-            put4(32 * i + 16 + 4 * c, transpose_halves(u[i].z, u[i].w, e));
+            put_pair(32 * i, transpose_halves(u[i].x, u[i].y, e), transpose_halves(u[i].z, u[i].w, e));
         } else if constexpr (!IS_V) {
             const u32x2 a = values(u[i].x), b = values(u[i].y), g = values(u[i].z), h = values(u[i].w);
             put8(8 * (8 * i + c), mk4(a.x, a.y, b.x, b.y));
             put8(8 * (8 * i + 4 + c), mk4(g.x, g.y, h.x, h.y));
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) put4(64 * i + 16 * k + 4 * c, values(transpose_bytes(u[i][k], e)));
+            for (int k = 0; k < 4; k += 2) put_pair(64 * i + 16 * k, values(transpose_bytes(u[i][k], e)), values(transpose_bytes(u[i][k + 1], e)));
         }
     }
 }
@@ -214,11 +218,20 @@ template <int DT>
 __global__ __launch_bounds__(64 * PAGE_WAVES) void k_kv_gather(const AttnDesc d, const GatherPlan plan, uint8_t *k_out, uint8_t *v_out) {
     constexpr int E = DT == PKV_BF16 ? 2 : 1;
     const PlanLanes<PKV_PLAN_FEW> lanes(plan.rows);
+    // the ranges' sequences and first tokens come with the plan, not behind it
+    uint32_t seqs[2], begins[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = (int)(threadIdx.x & 63) + 64 * k, at = i < PKV_PLAN_FEW ? i : PKV_PLAN_FEW - 1;
+        seqs[k] = (uint32_t)plan.at[at].seq;
+        begins[k] = (uint32_t)plan.at[at].begin;
+    }
+    asked_for();
     const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * PAGE_WAVES + (threadIdx.x >> 6)));
     const int which = x & 1, hp = x >> 1, unit = hp / d.Hkv, h = hp - unit * d.Hkv;
     if ((uint32_t)unit >= lanes.units(plan.rows)) return;            // the last work-group may have waves to spare
     const PlanUnit pu = lanes.find(plan.rows, (uint32_t)unit);       // (pu.seq: its place in the list)
-    const int seq = plan.at[pu.seq - plan.rows.seq0].seq, begin = plan.at[pu.seq - plan.rows.seq0].begin, end = begin + pu.rows;
+    const int place = pu.seq - plan.rows.seq0, seq = (int)lanes.pick(seqs, place), begin = (int)lanes.pick(begins, place), end = begin + pu.rows;
     const int page = begin / PKV_T + pu.unit;
     const int lo = begin > page * PKV_T ? begin : page * PKV_T, hi = end < (page + 1) * PKV_T ? end : (page + 1) * PKV_T;
     const uint32_t id = (uint32_t)PKV_CONST(int32_t, d.table)[(size_t)seq * d.row_stride + page];
