@@ -178,10 +178,11 @@ __global__ __launch_bounds__(64 * PAGE_WAVES) void k_kv_append_chunk(const AttnD
 // the bytes (four heads a wave, all asked for at once: 9.7).
 template <int D, int DT, bool IS_V>
 __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, uint8_t *out, size_t stride, int s0, int s1) {
-    const int lane = threadIdx.x & 63, t = IS_V ? lane & 15 : lane >> 2, c = IS_V ? lane >> 4 : lane & 3, G = t >> 2, e = t & 3;
+    // K: token t, a quad's four lanes side by side.  V: element 4 c + r of tokens 4 G .. 4 G + 3, then elements 4 c .. + 3 of token 4 G + r.
+    const int lane = threadIdx.x & 63, c = lane & 3, G = lane >> 2 & 3, r = lane >> 4, t = IS_V ? 4 * G + r : lane >> 2;
     constexpr int N = DT == PKV_BF16 ? D / 32 : D / 64;
     u32x4 u[N];
-    const u32x4 *unit = reinterpret_cast<const u32x4 *>(tile + (IS_V ? (G * 16 + 4 * c + e) * 16 : (c * 16 + t) * 16));
+    const u32x4 *unit = reinterpret_cast<const u32x4 *>(tile + (IS_V ? (G * 16 + 4 * c + r) * 16 : (c * 16 + t) * 16));
 #pragma unroll
     for (int i = 0; i < N; ++i) u[i] = unit[64 * i];
     const bool mine = t >= s0 && t < s1;
@@ -191,25 +192,33 @@ __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, ui
         return mk2(pack_bf16_rne(a[0] * scale, a[1] * scale), pack_bf16_rne(b[0] * scale, b[1] * scale));
     };
     auto put8 = [&](int at, u32x4 w) __attribute__((always_inline)) { if (mine) *reinterpret_cast<u32x4 *>(row + 2 * at) = w; };
-    // elements at + 4 c .. + 3 (lo) and at + 16 + 4 c .. + 3 (hi): lanes c and c ^ 1 exchange, so that either has eight in a row
+    // four tokens of element r of a group as 16-bit values -> four elements of token r, between the four rows of 16 lanes
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    auto turned = [&](u32x2 w) __attribute__((always_inline)) {
+        const u2 a = __builtin_amdgcn_permlane32_swap(w.x, w.y, false, false);         // now two tokens of elements r & 1 and 2 + (r & 1)
+        const u2 b = __builtin_amdgcn_permlane16_swap(__builtin_amdgcn_perm(a.y, a.x, 0x05040100u), __builtin_amdgcn_perm(a.y, a.x, 0x07060302u), false, false);
+        return mk2(__builtin_amdgcn_perm(b.y, b.x, 0x05040100u), __builtin_amdgcn_perm(b.y, b.x, 0x07060302u));
+    };
+    // elements at + 4 c .. + 3 (lo) and at + 16 + 4 c .. + 3 (hi): neighbours exchange, so that either has eight in a row
     auto put_pair = [&](int at, u32x2 lo, u32x2 hi) __attribute__((always_inline)) {
-        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-        const u2 a = __builtin_amdgcn_permlane16_swap(lo.x, hi.x, false, false), b = __builtin_amdgcn_permlane16_swap(lo.y, hi.y, false, false);
-        put8(at + 16 * (c & 1) + 8 * (c >> 1), mk4(a.x, b.x, a.y, b.y));
+        const bool odd = c & 1;
+        auto other = [&](uint32_t x) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false); };
+        const uint32_t x = other(odd ? lo.x : hi.x), y = other(odd ? lo.y : hi.y);
+        put8(at + 16 * (c & 1) + 8 * (c >> 1), odd ? mk4(x, y, hi.x, hi.y) : mk4(lo.x, lo.y, x, y));
     };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if constexpr (DT == PKV_BF16 && !IS_V) {
             put8(8 * (4 * i + c), u[i]);
         } else if constexpr (DT == PKV_BF16) {
-            put_pair(32 * i, transpose_halves(u[i].x, u[i].y, e), transpose_halves(u[i].z, u[i].w, e));
+            put_pair(32 * i, turned(mk2(u[i].x, u[i].y)), turned(mk2(u[i].z, u[i].w)));
         } else if constexpr (!IS_V) {
             const u32x2 a = values(u[i].x), b = values(u[i].y), g = values(u[i].z), h = values(u[i].w);
             put8(8 * (8 * i + c), mk4(a.x, a.y, b.x, b.y));
             put8(8 * (8 * i + 4 + c), mk4(g.x, g.y, h.x, h.y));
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; k += 2) put_pair(64 * i + 16 * k, values(transpose_bytes(u[i][k], e)), values(transpose_bytes(u[i][k + 1], e)));
+            for (int k = 0; k < 4; k += 2) put_pair(64 * i + 16 * k, turned(values(u[i][k])), turned(values(u[i][k + 1])));
         }
     }
 }
