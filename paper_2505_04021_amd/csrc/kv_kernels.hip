@@ -171,11 +171,12 @@ __global__ __launch_bounds__(64 * PAGE_WAVES) void k_kv_append_chunk(const AttnD
 }
 
 // kv_gather: cached tokens of several sequences as packed bf16 rows, the way back of kv_append_chunk.  One wave per (sequence, page its
-// range touches, kv head, K or V): whole 16-byte units are read as they lie, 1 KiB a request, V units are transposed between the lanes
-// of a quad, and rows leave in pieces of 8 or 16 bytes, 64 side by side.  Codes are decoded, multiplied by their block's scale in fp32 and
-// rounded to bf16 once.  Bound by memory, every byte once, and for short ranges by its dependent trips (plan, block id, page): 8192 tokens of
-// 8/128 bf16 13.6 us (67 MB, 4.9 TB/s; a large copy 5.1); 24 ragged ranges of e4m3 caches with 64-wide heads (27 MB) 8.7, of which 5.2 for
-// the bytes (four heads a wave, all asked for at once: 9.7).
+// range touches, kv head, K or V): whole 16-byte units are read, 1 KiB a request, V units are transposed between the wave's rows of 16
+// lanes, and every lane stores pieces of 16 bytes, a quad's four side by side.  Codes are decoded, multiplied by their block's scale in fp32
+// and rounded to bf16 once.  Bound by memory, every byte once, and for short ranges by its dependent trips (plan, block id, page): 8192
+// tokens of 8/128 bf16 12.1 us (67 MB, 5.5 TB/s), 24 ragged ranges of e4m3 caches with 64-wide heads (27 MB) 7.2, of which 5.2 for the bytes.
+// Stores count by requests: with V in pieces of 8 bytes and the lanes of a quad in four rows 13.9 and 8.2, in pieces of 16 12.8 and 7.3, K's lanes four
+// to a row 12.3 and 7.1.  Four heads a wave, all asked for at once, took 1 us more.
 template <int D, int DT, bool IS_V>
 __device__ __forceinline__ void gather_page(const uint8_t *tile, float scale, uint8_t *out, size_t stride, int s0, int s1) {
     // K: token t, a quad's four lanes side by side.  V: element 4 c + r of tokens 4 G .. 4 G + 3, then elements 4 c .. + 3 of token 4 G + r.

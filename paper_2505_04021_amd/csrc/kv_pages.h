@@ -157,6 +157,19 @@ __device__ __forceinline__ u32x2 transpose_halves(uint32_t w0, uint32_t w1, int 
     return mk2(__builtin_amdgcn_perm(z1, z0, sel), __builtin_amdgcn_perm(z3, z2, sel));
 }
 
+// V rows of bf16 values travel in pieces of 16 bytes: lanes c and c ^ 1 read one each, at pair_piece(c) of 32 elements, and exchange halves once they
+// are there, so that lane c has elements 4 c .. + 3 (two words) and 16 + 4 c .. + 3.  (With pieces of 8
+// bytes, twice the requests: us, kv_append of 2 x 32 rows into e4m3 caches 9.7, 9.2; kv_write of a row 25.5, 25.1.)
+__device__ __forceinline__ int pair_piece(int c) { return 16 * (c & 1) + 8 * (c >> 1); }
+__device__ __forceinline__ void exchange_pair(uint32_t *w) {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    const u2 a = __builtin_amdgcn_permlane16_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane16_swap(w[1], w[3], false, false);
+    w[0] = a.x;
+    w[1] = b.x;
+    w[2] = a.y;
+    w[3] = b.y;
+}
+
 // A V unit holds the four tokens of slots 4 * group .. + 3; those of slots first .. last - 1 are stored.  A unit that
 // is written in part is stored by elements and never read back: another call, on another stream, may be writing the other
 // tokens of the group.  e4m3: word u, byte k = token k of element 16 u; bf16: two words, then two words, two tokens each.
@@ -203,8 +216,7 @@ __device__ __forceinline__ void page_bf16(const TILE_OF &tile_of, const PageRows
             if constexpr (!IS_V) {
                 row_bytes<16, 2, decltype(a)::value>(w[i], p, t, 16 * (4 * i + c));
             } else {
-                row_bytes<8, 2, decltype(a)::value>(w[i], p, t, 2 * (32 * i + 4 * c));
-                row_bytes<8, 2, decltype(a)::value>(w[i] + 2, p, t, 2 * (32 * i + 16 + 4 * c));
+                row_bytes<16, 2, decltype(a)::value>(w[i], p, t, 2 * (32 * i + pair_piece(c)));
             }
         }
     });
@@ -218,6 +230,7 @@ __device__ __forceinline__ void page_bf16(const TILE_OF &tile_of, const PageRows
         if constexpr (!IS_V) {
             if (t >= p.s0 && t < p.s0 + p.n) *reinterpret_cast<u32x4 *>(tile + ((4 * i + c) * 16 + t) * 16) = mk4(w[i][0], w[i][1], w[i][2], w[i][3]);
         } else {
+            exchange_pair(w[i]);
             const u32x2 ta = transpose_halves(w[i][0], w[i][1], e), tb = transpose_halves(w[i][2], w[i][3], e);
             put_v_unit<2>(tile + ((i * 4 + G) * 16 + 4 * c + e) * 16, mk4(ta.x, ta.y, tb.x, tb.y), G, p.s0, p.s0 + p.n);
         }
@@ -351,7 +364,7 @@ __device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const Page
                 row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 4, p, t, 16 * (8 * i + 4 + c));
             } else {                                     // elements 64 i + 16 u + 4 c .. + 3
 #pragma unroll
-                for (int u = 0; u < 4; ++u) row_bytes<8, 2, decltype(a)::value>(x + 8 * i + 2 * u, p, t, 2 * (64 * i + 16 * u + 4 * c));
+                for (int u = 0; u < 4; u += 2) row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 2 * u, p, t, 2 * (64 * i + 16 * u + pair_piece(c)));
             }
         }
     });
@@ -361,6 +374,10 @@ __device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const Page
     uint8_t *tile = tile_of(scale_p);
     if (!tile) return;
     if constexpr (!IS_V) turn.turn(x);
+    else {
+#pragma unroll
+        for (int i = 0; i < NW / 2; ++i) exchange_pair(x + 4 * i);
+    }
     // what the tile holds: codes of the slots before
     u32x4 old[D / 64];
     u32x4 *unit = reinterpret_cast<u32x4 *>(tile + (IS_V ? (G * 16 + 4 * c + e) * 16 : (c * 16 + t) * 16));

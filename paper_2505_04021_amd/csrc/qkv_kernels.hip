@@ -406,9 +406,9 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
     }
 }
 
-// Bound by memory: ragged prompts of 4300 tokens of 32/8/128, neighbours as pairs, 115 MB, cold: 27.1 us (22.6 at a large copy's rate; 25.8 with
-// neither norm nor rotation).  39.0 with every head's weights and angles looked up and worked out by themselves, one row in flight a wave;
+// Bound by memory: ragged prompts of 4300 tokens of 32/8/128, neighbours as pairs, 115 MB, cold: 26.1 us (22.6 at a large copy's rate).  39.0 with every head's weights and angles looked up and worked out by themselves, one row in flight a wave;
 // with registers for five waves a SIMD instead of four 32.4, for three 28.9.  2400 tokens into an e4m3 cache 14.5 (before 23.5).
+// With V read in pieces of 8 bytes 26.5.
 // A prefill chunk.  Waves of whole pages as in k_kv_append_chunk (one per page that the chunk touches, kv head, and K or V), then waves for
 // the queries, each with some heads of one token.
 constexpr int QKV_WAVES = 4;
