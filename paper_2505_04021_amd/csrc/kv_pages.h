@@ -159,7 +159,7 @@ __device__ __forceinline__ u32x2 transpose_halves(uint32_t w0, uint32_t w1, int 
 
 // V rows of bf16 values travel in pieces of 16 bytes: lanes c and c ^ 1 read one each, at pair_piece(c) of 32 elements, and exchange halves once they
 // are there, so that lane c has elements 4 c .. + 3 (two words) and 16 + 4 c .. + 3.  (With pieces of 8
-// bytes, twice the requests: us, kv_append of 2 x 32 rows into e4m3 caches 9.7, 9.2; kv_write of a row 25.5, 25.1.)
+// bytes, twice the requests: us, kv_append_chunk of 8 x 512 tokens into an e4m3 cache of 8/128 9.7, 9.2; kv_write of 8192 tokens in bf16 25.5, 25.1.)
 __device__ __forceinline__ int pair_piece(int c) { return 16 * (c & 1) + 8 * (c >> 1); }
 __device__ __forceinline__ void exchange_pair(uint32_t *w) {
     typedef uint32_t u2 __attribute__((ext_vector_type(2)));
