@@ -410,7 +410,8 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
 // with registers for five waves a SIMD instead of four 32.4, for three 28.9.  2400 tokens into an e4m3 cache 14.5 (before 23.5).
 // With V read in pieces of 8 bytes 26.5.
 // A prefill chunk.  Waves of whole pages as in k_kv_append_chunk (one per page that the chunk touches, kv head, and K or V), then waves for
-// the queries, each with some heads of one token.
+// the queries, each with some heads of one token.  (Queries first: the prompts above 29.6 us, 27.5 so; 2000 tokens into an e4m3 cache, with their way
+// back, 21.0, 19.6.)
 constexpr int QKV_WAVES = 4;
 
 template <int D, int DT, int SEQS>
