@@ -445,9 +445,9 @@ __device__ __forceinline__ void attn_part(const AttnDesc &d, int wg, float *s_ac
     }
     const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
     if (part >= n_parts) {
-        if (!JOIN && (int)threadIdx.x < g) {
-            at_part->sums[threadIdx.x * (D + 4) + D] = -INFINITY;
-            at_part->sums[threadIdx.x * (D + 4) + D + 1] = 0.f;
+        if constexpr (!JOIN) {                            // (the join takes every part as it is, without a weight for those not written)
+            for (int i = threadIdx.x; i < g * (D / 4 + 1); i += 64 * SMALL_WAVES)
+                *reinterpret_cast<f32x4 *>(at_part->sums + 4 * i) = f32x4{i % (D / 4 + 1) == D / 4 ? -INFINITY : 0.f, 0.f, 0.f, 0.f};
         }
         return;
     }

@@ -184,15 +184,21 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
         }
     };
     sums(0);
-    m[0] = lane < parts ? m[0] : -INFINITY;
-    m[1] = lane < own_parts ? m[1] : -INFINITY;
+    if (lane >= parts) {
+        m[0] = -INFINITY;
+        l[0] = 0.f;
+    }
+    if (lane >= own_parts) {
+        m[1] = -INFINITY;
+        l[1] = 0.f;
+    }
     float M = fmaxf(m[0], m[1]), den = 0.f;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         m[k] = merge_weight(m[k], M);
-        den += m[k] != 0.f ? l[k] * m[k] : 0.f;
+        den += l[k] * m[k];                                // (a part that weighs nothing may still be NaN: it had a NaN logit, or a NaN among its values)
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
@@ -203,18 +209,16 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_prefix_join(const AttnDesc 
         for (int k = 0; k < TRIP; ++k) {
             const int p = p0 + SIDE * k + side;
             const float a = __shfl(m[0], p & 63), c = __shfl(m[1], (p - parts) & 63), weight = p < parts ? a : (p < all ? c : 0.f);
-            if (weight != 0.f) acc += v[k] * weight;       // (what weighs nothing may not have been written)
+            if (p < all) acc += v[k] * weight;
         }
     }
 #pragma unroll
     for (int o = QUADS; o < 64; o <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
-    // a row that sees nothing is defined as zero, and so is one whose prefix is not there
-    if (!(den != 0.f) || there < blocks) {
-        acc = f32x4{0.f, 0.f, 0.f, 0.f};
-        den = 1.f;
-    }
+    // a row that sees nothing is defined as zero (its sums are), and so is one whose prefix is not there
+    if (there < blocks) acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (den == 0.f || there < blocks) den = 1.f;
     if (side == 0) *reinterpret_cast<f32x4 *>(d.out + ((size_t)seq * d.Hq + hq) * D + 4 * quad) = acc * (1.0f / den);
 }
 
