@@ -121,7 +121,8 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
 
 
 # Calls of few tokens take the host longer than the GPU: their addresses go as plain integers and their host lists as bytes, not as c_void_p and numpy
-# arrays' addresses (qkv_append 4.8 us without the library's part before, decode_attention_prefix 4.7, kv_gather 6.0; 4.0, 1.9 and 2.4 so).
+# arrays' addresses (qkv_append 4.8 us without the library's part before, decode_attention_prefix 4.7, kv_gather 6.0; 4.0, 1.9 and 2.4 so;
+# qkv_append's look at what its tensors hold, in _qkv, takes 0.7 more).
 def _at(tensor):
     return None if tensor is None else tensor.data_ptr()
 
@@ -172,6 +173,16 @@ def rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, train
     return out
 
 
+def _rows(x, heads, d, dtypes):
+    """Address, distance and number of tokens whose heads lie side by side."""
+    n, h, e = x.shape
+    token, head, one = x.stride()
+    if h != heads or e != d or one != 1 or (head != d and h != 1) or x.dtype not in dtypes:
+        raise ValueError(f"bf16 [tokens][{heads}][{d}] with a token's heads side by side, not {x.dtype} {tuple(x.shape)} of strides {x.stride()}")
+    # (0 says "packed" to the library: tokens that all lie in one place go as a distance that it refuses)
+    return x.data_ptr(), (token or 1) if n > 1 else 0, n
+
+
 class PrismKV:
     """One per process; the library holds global pool / model tables."""
 
@@ -185,6 +196,7 @@ class PrismKV:
         self.device = torch.device(device)
         self.lib = _load()
         self._shape = {}
+        self._bf16 = frozenset((torch.bfloat16, torch.int16, torch.uint16))     # values, or their bits
         self._keep = {}
         self.use_current_stream()
 
@@ -420,29 +432,46 @@ class PrismKV:
     def rotary_destroy(self, rotary):
         return self.lib.rotary_destroy(rotary)
 
-    @staticmethod
-    def _rows(x, heads, d):
-        """Address and distance of tokens whose heads lie side by side."""
-        n, h, e = x.shape
-        token, head, one = x.stride()
-        assert h == heads and e == d and one == 1 and (head == d or h == 1) and x.element_size() == 2
-        return x.data_ptr(), token if n > 1 else 0
-
-    def _qkv(self, model, q, k, v, q_weight, k_weight, eps, rotary, before):
+    def _qkv(self, model, batch, tokens, q_out, q, k, v, q_weight, k_weight, eps, rotary, before):
+        """The call's pkv_qkv; None, which the library refuses behind what it looks at first, where a tensor holds less than the call would read or write."""
+        if model not in self._shape:
+            return None
         hq, hkv, d, _ = self._shape[model]
-        (q, qs), (k, ks), (v, vs) = self._rows(q, hq, d), self._rows(k, hkv, d), self._rows(v, hkv, d)
-        return _QKV.pack(q, k, v, qs, ks, vs, _at(q_weight) or 0, _at(k_weight) or 0, eps, rotary, _at(before) or 0)
+        bf16 = self._bf16
+        q, qs, nq = _rows(q, hq, d, bf16)
+        k, ks, nk = _rows(k, hkv, d, bf16)
+        v, vs, nv = _rows(v, hkv, d, bf16)
+        if nq < tokens or nk < tokens or nv < tokens or q_out is None or q_out.nbytes < 2 * tokens * hq * d or not q_out.is_contiguous():
+            return None
+        qw = kw = at = 0
+        if q_weight is not None:
+            if q_weight.nbytes != 2 * d or not q_weight.is_contiguous():
+                return None
+            qw = q_weight.data_ptr()
+        if k_weight is not None:
+            if k_weight.nbytes != 2 * d or not k_weight.is_contiguous():
+                return None
+            kw = k_weight.data_ptr()
+        if before is not None:
+            if before.nbytes < 4 * batch or not before.is_contiguous():
+                return None
+            at = before.data_ptr()
+        return _QKV.pack(q, k, v, qs, ks, vs, qw, kw, eps, rotary, at)
 
     def qkv_append_dev(self, model, q, k, v, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
-        """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues."""
-        x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append(model, ctx_lens.numel(), x, _at(ctx_lens), _at(q_out))
+        """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues.  Rows beyond B are not looked at;
+        fewer are refused (PKV_E_ARG), and so are tokens that share their memory (a broadcast axis)."""
+        n = ctx_lens.numel()
+        x = self._qkv(model, n, n, q_out, q, k, v, q_weight, k_weight, eps, rotary, before)
+        return self.lib.qkv_append(model, n, x, ctx_lens.data_ptr(), q_out.data_ptr() if x else None)
 
     def qkv_append_chunk_dev(self, model, q, k, v, q_lens, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """The same for packed chunks; q_lens: list or host int32 array.  Only enqueues."""
         ql = _i32(q_lens)
-        x = self._qkv(model, q, k, v, q_weight, k_weight, eps, rotary, before)
-        return self.lib.qkv_append_chunk(model, len(ql) // 4, x, ql, _at(ctx_lens), _at(q_out))
+        n = len(ql) // 4
+        tokens = sum(memoryview(ql).cast("i")) if n <= 64 else int(np.frombuffer(ql, dtype=np.int32).sum(dtype=np.int64))
+        x = self._qkv(model, n, tokens, q_out, q, k, v, q_weight, k_weight, eps, rotary, before) if ctx_lens.numel() >= n else None
+        return self.lib.qkv_append_chunk(model, n, x, ql, ctx_lens.data_ptr(), q_out.data_ptr() if x else None)
 
     def kv_read(self, model, seq, tok_begin, n_tok):
         """-> (code, k, v, k_scale, v_scale) as numpy: elements [n_tok][Hkv][D], scales [n_tok][Hkv] (None for bf16)."""

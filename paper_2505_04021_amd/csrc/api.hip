@@ -1922,7 +1922,7 @@ int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_l
     if (!m) return PKV_E_HANDLE;
     if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
     if (batch == 0) return 0;
-    if (!in || !q_lens || !ctx_lens) return PKV_E_ARG;
+    if (!q_lens || !ctx_lens) return PKV_E_ARG;
     int64_t total = 0;
     for (int s = 0; s < batch; ++s) {
         if (q_lens[s] < 0) return PKV_E_ARG;
@@ -1930,6 +1930,7 @@ int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_l
         if (total > (int64_t)1 << 24) return PKV_E_RANGE;
     }
     if (total == 0) return 0;
+    if (!in) return PKV_E_ARG;
     QkvArgs a{};
     const int rc = fill_qkv(a, *m, *in, q_out);
     if (rc) return rc;
