@@ -247,9 +247,10 @@ int kv_append_chunk(int model, int batch, const void *k_new, const void *v_new, 
 /* Rotary positions.  Elements 0 .. rot_dim - 1 of a head form rot_dim / 2 pairs; pair i turns by
  * inv_freq[i] radians a token, (a, b) -> magnitude * (a cos - b sin, b cos + a sin), and the
  * elements from rot_dim on stay as they are.  PKV_ROTARY_HALF: pair i is elements i and
- * i + rot_dim / 2; PKV_ROTARY_PAIRS: elements 2 i and 2 i + 1.  Angles are exact to 2^-32 of a
- * circle at every int32 position (the frequencies are kept as 64-bit fractions of a circle).
- * rotary_create takes the frequencies (HOST double [rot_dim / 2], finite, rot_dim even, 2 .. 128),
+ * i + rot_dim / 2; PKV_ROTARY_PAIRS: elements 2 i and 2 i + 1.  Angles are worked out to 2^-31 of a
+ * circle at every int32 position, for frequencies up to 2^32 radians (which are kept as 64-bit fractions
+ * of a circle); sine and cosine are the hardware's, of the angle rounded to 24 bits (2^-26 of a circle at most).
+ * rotary_create takes the frequencies (HOST double [rot_dim / 2], below 2^64 in magnitude, rot_dim even, 2 .. 128),
  * so any rule of scaling them can be used; it returns an id (lowest unused, 0 .. 63) that any
  * model and layer may use, PKV_E_NOMEM beyond.  rotary_destroy waits for the device; graphs
  * captured with the id must not be replayed afterwards.

@@ -83,6 +83,9 @@ int pkv_tune_xcd(int updates);
 /* Host-side check of the multiply-shift division the kernels use to split a block
  * id into (frame, slot): returns n / d computed that way. */
 uint32_t pkv_debug_fastdiv(uint32_t n, uint32_t d);
+/* Host-side check of the fractions of a circle that rotary_create keeps: |radians| < 2^64 in 2^-64 of a circle,
+ * modulo one. */
+uint64_t pkv_debug_circle_fraction(double radians);
 /* Test hook for the out-of-memory path of elastic pools: after `after` more successful frame
  * mappings the next one is refused as if the driver had no memory left, once (-1 = never). */
 int pkv_debug_fail_frame_map(int after);

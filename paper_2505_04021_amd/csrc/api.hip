@@ -263,12 +263,24 @@ struct Rotary {
 Rotary g_rotary[PKV_MAX_ROTARY];
 constexpr int64_t kQueryWaves = 4096;     // waves for queries that a launch of qkv_append_chunk has at least, where there are as many
 
-
-// An angle as a fraction of a circle, in 2^-64 of one: |radians| / 2 pi modulo 1, to the 53 bits of the quotient.
+// An angle as a fraction of a circle, to the nearest 2^-64 of one: the 53 bits of the angle times 128 of 1 / 2 pi, in integers.  A position of
+// 31 bits multiplies what is lost here, so that it has to be less than a double keeps: a fraction of 53 bits, as the quotient in doubles is, put angles at
+// 2^31 off by 2^-25 of a circle for frequencies around 1.  |radians| < kMaxFrequency; up to 2^32 the constant's own end does not show.
+constexpr double kMaxFrequency = 0x1p64;
 uint64_t circle_fraction(double radians) {
-    double whole;
-    const double f = modf(fabs(radians) * 0.15915494309189533577, &whole);
-    const uint64_t x = f >= 1.0 ? 0 : (uint64_t)ldexp(f, 64);
+    constexpr uint64_t kHigh = 0xa2f9836e4e441529u, kLow = 0xfc2757d1f534ddc1u;      // 2^130 / 2 pi
+    int e;
+    const uint64_t m = (uint64_t)ldexp(frexp(fabs(radians), &e), 53);
+    // m * constant, 181 bits, in units of 2^(e - 183) of a circle
+    const unsigned __int128 low = (unsigned __int128)m * kLow, high = (unsigned __int128)m * kHigh + (uint64_t)(low >> 64);
+    const uint64_t word[3] = {(uint64_t)low, (uint64_t)high, (uint64_t)(high >> 64)};
+    auto from_bit = [&](int b) -> uint64_t {
+        if (b >= 192) return 0;
+        const int i = b / 64, s = b % 64;
+        return word[i] >> s | (s > 0 && i < 2 ? word[i + 1] << (64 - s) : 0);
+    };
+    const int unit = 119 - e;                             // the bit that stands for 2^-64 of a circle; at least 55
+    const uint64_t x = from_bit(unit) + (from_bit(unit - 1) & 1);
     return radians < 0.0 ? 0 - x : x;
 }
 
@@ -869,6 +881,8 @@ int pkv_debug_fail_frame_map(int after) {
     g_fail_map_after = after;
     return PKV_OK;
 }
+
+uint64_t pkv_debug_circle_fraction(double radians) { return fabs(radians) < kMaxFrequency ? circle_fraction(radians) : 0; }
 
 uint32_t pkv_debug_fastdiv(uint32_t n, uint32_t d) {
     if (d == 0) return 0;
@@ -1829,7 +1843,7 @@ int rotary_create(int rot_dim, int layout, const double *inv_freq, double magnit
     if (!isfinite(magnitude) || !isfinite((float)magnitude)) return PKV_E_ARG;
     uint64_t turns[64] = {};
     for (int i = 0; i < rot_dim / 2; ++i) {
-        if (!isfinite(inv_freq[i])) return PKV_E_ARG;
+        if (!(fabs(inv_freq[i]) < kMaxFrequency)) return PKV_E_ARG;
         turns[i] = circle_fraction(inv_freq[i]);
     }
     int id = -1;

@@ -8,8 +8,10 @@
 // be had the caller rotated and rounded first.
 //
 // Angles: position * frequency is off by whole radians in fp32 long before contexts end (2^20 tokens: 2^-4 of a radian), so a
-// frequency is held as a fraction of a circle in 64 bits and multiplied by the position modulo one circle, in integers: exact to
-// 2^-32 of a circle at any position, and what v_sin_f32 and v_cos_f32 take as their argument.
+// frequency is held as a fraction of a circle in 64 bits, to the nearest, and multiplied by the position modulo one circle, in integers: within
+// 2^-31 of a circle at any position.  v_sin_f32 and v_cos_f32 take that fraction in fp32, 2^-26 of a circle off at most (near half of one); with
+// their own error, 2^-22.9 at most over 2^24 fractions of a circle, sine and cosine are 2^-22 off: below what the rounding to bf16 leaves, 2^-8 of an
+// outcome, except where a and b all but cancel.
 #include "kv_pages.h"
 
 namespace {
