@@ -274,7 +274,8 @@ int rotary_destroy(int rotary);
  * into the cache.  Per head x of head_dim elements, in fp32: y = x / sqrt(mean(x^2) + eps) * weight
  * where there is a weight, then the rotation, then one rounding to bf16 (to nearest even).  Keys so
  * rounded, and values as they came, go into the cache exactly as kv_append / kv_append_chunk would put them
- * there, scales and codes of e4m3 models included.
+ * there, scales and codes of e4m3 models included.  A token's key and query are the same to the bit by either
+ * call, however the chunks are cut.
  *   q, k, v     dev, bf16; a token's q_heads (kv_heads) heads of head_dim elements lie side by side,
  *               and tokens are *_stride elements apart (0: packed), so all three may be parts of
  *               one fused projection.  16-byte aligned rows are read faster; any alignment works.

@@ -69,7 +69,54 @@ __device__ __forceinline__ float square_sum(const uint32_t *w) {
     for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
     return sum;
 }
-__device__ __forceinline__ float norm_of(float squares, int width, float eps) { return __builtin_amdgcn_rsqf(squares / (float)width + eps); }
+// (per: 1 / width, a power of two)
+__device__ __forceinline__ float norm_of(float squares, float per, float eps) {
+#pragma clang fp contract(off)
+    return __builtin_amdgcn_rsqf(squares * per + eps);
+}
+
+// Keys come by three ways (a lane with two elements of a token's head in a decode step, with groups of eight in a chunk, both of a pair or one of them), and are
+// the same to the bit by all of them: what a token leaves in the cache does not depend on the call that brought it.  So every product and sum of
+// theirs is written out here, none fused by the compiler, and the squares of a head are summed in one order: by the bits of their places, 6, 5, 0, 1, 2, 3, 4.
+
+// x, p: an element and its partner as they came, w, pw: their weights, r: the head's norm (1 where there is none)
+__device__ __forceinline__ float normed_key(float x, float r, float w) {
+#pragma clang fp contract(off)
+    return (x * r) * w;
+}
+// an element's outcome from it and its partner, both normed; sn: negative for the first of a pair
+__device__ __forceinline__ float turned_key(float x, float p, float sn, float cs) {
+#pragma clang fp contract(off)
+    return __builtin_fmaf(x, cs, p * sn);
+}
+// of groups of eight elements, D / 32 of them 32 elements apart: the sum over this lane's; the lanes l, l ^ 16, l ^ 32, l ^ 48 have the others
+template <int D>
+__device__ __forceinline__ float key_squares(const uint32_t *words) {
+#pragma clang fp contract(off)
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float q[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            const float x = i & 1 ? bf16_hi(words[4 * j + i / 2]) : bf16_lo(words[4 * j + i / 2]);
+            q[j] = x * x;
+        }
+        if constexpr (D == 128) s[i] = (q[0] + q[2]) + (q[1] + q[3]);
+        else s[i] = q[0] + q[1];
+    }
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+}
+// of elements `lane` and, of 128, lane + 64: the sum over all of the head
+__device__ __forceinline__ float key_squares_by_lane(float x0, float x1, bool wide) {
+#pragma clang fp contract(off)
+    const float a = x0 * x0, b = x1 * x1;
+    float s = wide ? a + b : a;
+    s = s + __shfl_xor(s, 32);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) s = s + __shfl_xor(s, o);
+    return s;
+}
 
 // What makes eight elements e0 .. e0 + 7 of a head's outcome at a position: x own + partner other, with the norm's weights and the magnitude in
 // it, the same for all heads.  An element that is not rotated has no partner: other = -0, and its partner is taken as 0, so that it stays
@@ -94,19 +141,10 @@ __device__ __forceinline__ void some_turns(uint64_t *t, const QkvArgs &a, int pa
     }
 }
 
+// The turns of elements e0 .. e0 + 7 (of pairs of neighbours: four) and, but for those, their partners' weights.
 template <bool PAIRS>
-__device__ __forceinline__ Factors factors(const QkvArgs &a, const uint16_t *weight, int e0, int pos, bool rotated) {
-    Factors f;
+__device__ __forceinline__ void turns_of_eight(uint64_t *turns, float *pw, const QkvArgs &a, const uint16_t *weight, int e0) {
     const int half = a.rot >> 1;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        f.own[i] = 1.f;
-        f.other[i] = -0.f;
-    }
-    if (weight) eight_weights(f.own, weight, e0);
-    if (!rotated) return f;
-    uint64_t turns[8];
-    float pw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) pw[i] = 1.f;
     if constexpr (PAIRS) some_turns<4>(turns, a, e0 >> 1);
@@ -122,6 +160,22 @@ __device__ __forceinline__ Factors factors(const QkvArgs &a, const uint16_t *wei
             if (weight) pw[i] = bf16_of(weight[partner_of(a, e)]);
         }
     }
+}
+
+template <bool PAIRS>
+__device__ __forceinline__ Factors factors(const QkvArgs &a, const uint16_t *weight, int e0, int pos, bool rotated) {
+    Factors f;
+    const int half = a.rot >> 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        f.own[i] = 1.f;
+        f.other[i] = -0.f;
+    }
+    if (weight) eight_weights(f.own, weight, e0);
+    if (!rotated) return f;
+    uint64_t turns[8];
+    float pw[8];
+    turns_of_eight<PAIRS>(turns, pw, a, weight, e0);
 #pragma unroll
     for (int i = 0; i < 8; i += PAIRS ? 2 : 1) {
         const int e = e0 + i;
@@ -149,6 +203,7 @@ __device__ __forceinline__ Factors factors(const QkvArgs &a, const uint16_t *wei
 // partners are among them); r: the head's norm, 1 without one.
 template <bool PAIRS>
 __device__ __forceinline__ u32x4 turned8(const Factors &f, const uint32_t *xw, const uint32_t *pw, int e0, int rot, float r) {
+#pragma clang fp contract(off)
     float x[8], p[8], y[8];
     widen(x, xw);
     if constexpr (PAIRS) {
@@ -156,7 +211,7 @@ __device__ __forceinline__ u32x4 turned8(const Factors &f, const uint32_t *xw, c
         for (int i = 0; i < 8; ++i) p[i] = e0 + i < rot ? x[i ^ 1] : 0.f;
     } else widen(p, pw);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (x[i] * r) * f.own[i] + (p[i] * r) * f.other[i];
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[i] * r, f.own[i], (p[i] * r) * f.other[i]);
     return mk4(pack_bf16_rne(y[0], y[1]), pack_bf16_rne(y[2], y[3]), pack_bf16_rne(y[4], y[5]), pack_bf16_rne(y[6], y[7]));
 }
 
@@ -199,7 +254,7 @@ struct TurnKeys {
     // groups j and k, pairs 8 (4 j + c) .. + 7: both outcomes
     __device__ __forceinline__ void both(uint32_t *words, int j, int k, float r) {
         const int e0 = 8 * (4 * j + c), e1 = 8 * (4 * k + c);
-        float x[8], y[8], u[8], v[8], wx[8], wy[8];
+        float x[8], y[8], wx[8], wy[8];
         widen(x, words + 4 * j);
         widen(y, words + 4 * k);
         uint64_t turns[8];
@@ -214,35 +269,53 @@ struct TurnKeys {
         for (int i = 0; i < 8; ++i) {
             float sn, cs;
             turn_of(turns[i], pos, sn, cs);
-            const float p = (x[i] * r) * wx[i], q = (y[i] * r) * wy[i];
+            const float p = normed_key(x[i], r, wx[i]), q = normed_key(y[i], r, wy[i]);
             sn *= a.magnitude;
             cs *= a.magnitude;
-            u[i] = p * cs - q * sn;
-            v[i] = q * cs + p * sn;
+            x[i] = turned_key(p, q, -sn, cs);
+            y[i] = turned_key(q, p, sn, cs);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            words[4 * j + i] = pack_bf16_rne(u[2 * i], u[2 * i + 1]);
-            words[4 * k + i] = pack_bf16_rne(v[2 * i], v[2 * i + 1]);
+            words[4 * j + i] = pack_bf16_rne(x[2 * i], x[2 * i + 1]);
+            words[4 * k + i] = pack_bf16_rne(y[2 * i], y[2 * i + 1]);
         }
+    }
+    // group j by itself
+    __device__ __forceinline__ void group(uint32_t *words, int j, float r, bool rotated) {
+        const int e0 = 8 * (4 * j + c), half = a.rot >> 1;
+        float x[8], w[8];
+        widen(x, words + 4 * j);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 1.f;
+        if (a.k_weight) eight_weights(w, a.k_weight, e0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = normed_key(x[i], r, w[i]);
+        if (rotated) {
+            uint64_t turns[8];
+            float p[8], pw[8];
+            turns_of_eight<PAIRS>(turns, pw, a, a.k_weight, e0);
+            if constexpr (!PAIRS) widen(p, px[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = PAIRS ? x[i ^ 1] : normed_key(p[i], r, pw[i]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = e0 + i;
+                float sn, cs;
+                turn_of(turns[PAIRS ? i >> 1 : i], pos, sn, cs);
+                sn *= a.magnitude;
+                cs *= a.magnitude;
+                const float y = turned_key(x[i], p[i], (PAIRS ? (i & 1) == 0 : e < half) ? -sn : sn, cs);
+                x[i] = e < a.rot ? y : x[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) words[4 * j + i] = pack_bf16_rne(x[2 * i], x[2 * i + 1]);
     }
     __device__ __forceinline__ void turn(uint32_t *words) {
         if (!a.turns && !a.k_weight) return;
         float r = 1.f;
-        if (a.k_weight) {
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) sum += square_sum(words + 4 * j);
-            r = norm_of(lanes4_sum(sum), D, a.eps);
-        }
-        auto group = [&](int j, bool rotated) __attribute__((always_inline)) {
-            const int e0 = 8 * (4 * j + c);
-            uint32_t none[4] = {0u, 0u, 0u, 0u};
-            const Factors f = factors<PAIRS>(a, a.k_weight, e0, pos, rotated);
-            const u32x4 y = turned8<PAIRS>(f, words + 4 * j, rotated && !PAIRS ? px[j] : none, e0, a.rot, r);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) words[4 * j + i] = y[i];
-        };
+        if (a.k_weight) r = norm_of(lanes4_sum(key_squares<D>(words)), 1.f / D, a.eps);
         if (!PAIRS && a.turns && near) {
             if (D == 128 && a.rot == 128) {
                 both(words, 0, D == 128 ? 2 : 1, r);
@@ -251,14 +324,14 @@ struct TurnKeys {
                 both(words, 0, 1, r);
                 if (D == 128 && a.k_weight) {
 #pragma unroll
-                    for (int j = 2; j < D / 32; ++j) group(j, false);
+                    for (int j = 2; j < D / 32; ++j) group(words, j, r, false);
                 }
             }
             return;
         }
         // (a condition for the whole wave: lanes of one group of eight differ in it only where rot is no multiple of 32)
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) group(j, a.turns && 32 * j < a.rot);
+        for (int j = 0; j < D / 32; ++j) group(words, j, r, a.turns && 32 * j < a.rot);
     }
 };
 
@@ -309,7 +382,7 @@ __device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a
                     }
                 } else partners_by_element(a, src + (live ? h : head0) * D, e0, pw);
             }
-            const float r = a.q_weight ? norm_of(head_sum<LANES>(square_sum(xw)), D, a.eps) : 1.f;
+            const float r = a.q_weight ? norm_of(head_sum<LANES>(square_sum(xw)), 1.f / D, a.eps) : 1.f;
             const u32x4 y = turned8<PAIRS>(f, xw, pw, e0, a.rot, r);
             if (live) *reinterpret_cast<u32x4 *>(dst + h * D + e0) = y;
         }
@@ -359,27 +432,23 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
         if (lane == 0) atomicOr(d.err, 1u);
         return;
     }
-    {
+    if (a.turns || a.k_weight) {
         float x[2] = {bf16_lo(kx[0]), bf16_lo(kx[1])}, p[2] = {bf16_lo(kp[0]), bf16_lo(kp[1])};
         float r = 1.f;
-        if (a.k_weight) {
-            float sum = x[0] * x[0] + (D > 64 ? x[1] * x[1] : 0.f);
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            r = norm_of(sum, D, a.eps);
-        }
+        if (a.k_weight) r = norm_of(key_squares_by_lane(x[0], x[1], D > 64), D > 64 ? 1.f / 128 : 1.f / 64, a.eps);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = i ? second : lane, pe = partner_of(a, e), half = a.rot >> 1;
             if (a.k_weight) {
-                x[i] *= r * bf16_of(a.k_weight[e]);
-                p[i] *= r * bf16_of(a.k_weight[pe]);
+                x[i] = normed_key(x[i], r, bf16_of(a.k_weight[e]));
+                p[i] = normed_key(p[i], r, bf16_of(a.k_weight[pe]));
             }
             if (a.turns && e < a.rot) {
                 const int pair = a.pairs ? e >> 1 : (e < half ? e : e - half);
                 float s, c;
                 turn_of(a.turns[pair], before + ctx - 1, s, c);
-                x[i] = x[i] * (c * a.magnitude) + p[i] * ((e < pe ? -s : s) * a.magnitude);
+                s *= a.magnitude;
+                x[i] = turned_key(x[i], p[i], e < pe ? -s : s, c * a.magnitude);
             }
             kx[i] = pack_bf16_rne(x[i], 0.f) & 0xffffu;
         }
