@@ -255,7 +255,8 @@ int kv_append_chunk(int model, int batch, const void *k_new, const void *v_new, 
  * model and layer may use, PKV_E_NOMEM beyond.  rotary_destroy waits for the device; graphs
  * captured with the id must not be replayed afterwards.
  * rotary_frequencies is a host call (no device work): inv_freq[i] = f_i = base^(-2 i / rot_dim), by
- * `scaling` changed for contexts `factor` times those of training; returns rot_dim / 2.
+ * `scaling` changed for contexts `factor` times those of training; returns rot_dim / 2
+ * (PKV_E_ARG, and nothing written, where a frequency or the base would leave the range of doubles).
  *   PKV_ROTARY_PLAIN   not changed (factor, trained, low and high are not looked at)
  *   PKV_ROTARY_LINEAR  f_i / factor: positions are squeezed
  *   PKV_ROTARY_BASE    base * factor^(rot_dim / (rot_dim - 2)) instead of base: the slowest pair

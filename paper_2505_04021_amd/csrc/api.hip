@@ -1818,12 +1818,14 @@ int rotary_frequencies(int rot_dim, double base, int scaling, double factor, dou
     if (rot_dim < 2 || (rot_dim & 1) || rot_dim > 128 || !inv_freq || !(base > 0.0) || !isfinite(base)) return PKV_E_ARG;
     if (scaling < PKV_ROTARY_PLAIN || scaling > PKV_ROTARY_RAMP) return PKV_E_ARG;
     if (scaling != PKV_ROTARY_PLAIN && !(factor > 0.0 && isfinite(factor))) return PKV_E_ARG;
-    if (scaling == PKV_ROTARY_RAMP && !(trained > 0.0 && isfinite(trained) && low < high && isfinite(low) && isfinite(high))) return PKV_E_ARG;
+    if (scaling == PKV_ROTARY_RAMP && !(trained > 0.0 && isfinite(trained) && low < high && isfinite(high - low))) return PKV_E_ARG;
     if (scaling == PKV_ROTARY_BASE) {
         if (rot_dim < 4) return PKV_E_ARG;                 // one pair, of frequency 1 whatever the base
         base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+        if (!(base > 0.0) || !isfinite(base)) return PKV_E_ARG;
     }
     const int n = rot_dim / 2;
+    double out[64];
     for (int i = 0; i < n; ++i) {
         double f = pow(base, -(double)i / n);
         if (scaling == PKV_ROTARY_LINEAR) f /= factor;
@@ -1832,8 +1834,10 @@ int rotary_frequencies(int rot_dim, double base, int scaling, double factor, dou
             keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
             f = f * keep + f / factor * (1.0 - keep);
         }
-        inv_freq[i] = f;
+        if (!isfinite(f)) return PKV_E_ARG;
+        out[i] = f;
     }
+    memcpy(inv_freq, out, n * sizeof(double));
     return n;
 }
 
