@@ -17,6 +17,7 @@ ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 
 # pkv_qkv: q, k, v, their strides, q_weight, k_weight, eps, rotary, before
 _QKV = struct.Struct("@PPPqqqPPfiP")
+_pack_qkv = _QKV.pack
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -123,7 +124,7 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
 
 # Calls of few tokens take the host longer than the GPU: their addresses go as plain integers and their host lists as bytes, not as c_void_p and numpy
 # arrays' addresses (qkv_append 4.8 us without the library's part before, decode_attention_prefix 4.7, kv_gather 6.0; 4.0, 1.9 and 2.4 so;
-# qkv_append's look at what its tensors hold, in _qkv, takes 0.7 more).
+# qkv_append's look at what its tensors hold, in _qkv, takes 0.4 more).
 def _at(tensor):
     return None if tensor is None else tensor.data_ptr()
 
@@ -174,14 +175,14 @@ def rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, train
     return out
 
 
-def _rows(x, heads, d, dtypes):
-    """Address, distance and number of tokens whose heads lie side by side."""
+def _row_distance(x, heads, d, dtypes):
+    """Distance of tokens whose heads lie side by side, as the library takes it, where a look at shape and strides did not settle it."""
     n, h, e = x.shape
     token, head, one = x.stride()
     if h != heads or e != d or one != 1 or (head != d and h != 1) or x.dtype not in dtypes:
         raise ValueError(f"bf16 [tokens][{heads}][{d}] with a token's heads side by side, not {x.dtype} {tuple(x.shape)} of strides {x.stride()}")
     # (0 says "packed" to the library: tokens that all lie in one place go as a distance that it refuses)
-    return x.data_ptr(), (token or 1) if n > 1 else 0, n
+    return (token or 1) if n > 1 else 0
 
 
 class PrismKV:
@@ -435,13 +436,24 @@ class PrismKV:
 
     def _qkv(self, model, batch, tokens, q_out, q, k, v, q_weight, k_weight, eps, rotary, before):
         """The call's pkv_qkv; None, which the library refuses behind what it looks at first, where a tensor holds less than the call would read or write."""
-        if model not in self._shape:
+        shape = self._shape.get(model)
+        if shape is None:
             return None
-        hq, hkv, d, _ = self._shape[model]
+        hq, hkv, d, _ = shape
         bf16 = self._bf16
-        q, qs, nq = _rows(q, hq, d, bf16)
-        k, ks, nk = _rows(k, hkv, d, bf16)
-        v, vs, nv = _rows(v, hkv, d, bf16)
+        # (written out: few tokens' calls take the host longer than the GPU)
+        nq, h, e = q.shape
+        qs, head, one = q.stride()
+        if not (qs and nq > 1 and h == hq and e == d == head and one == 1 and q.dtype in bf16):
+            qs = _row_distance(q, hq, d, bf16)
+        nk, h, e = k.shape
+        ks, head, one = k.stride()
+        if not (ks and nk > 1 and h == hkv and e == d == head and one == 1 and k.dtype in bf16):
+            ks = _row_distance(k, hkv, d, bf16)
+        nv, h, e = v.shape
+        vs, head, one = v.stride()
+        if not (vs and nv > 1 and h == hkv and e == d == head and one == 1 and v.dtype in bf16):
+            vs = _row_distance(v, hkv, d, bf16)
         if nq < tokens or nk < tokens or nv < tokens or q_out is None or q_out.nbytes < 2 * tokens * hq * d or not q_out.is_contiguous():
             return None
         qw = kw = at = 0
@@ -457,7 +469,7 @@ class PrismKV:
             if before.nbytes < 4 * batch or not before.is_contiguous():
                 return None
             at = before.data_ptr()
-        return _QKV.pack(q, k, v, qs, ks, vs, qw, kw, eps, rotary, at)
+        return _pack_qkv(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, qw, kw, eps, rotary, at)
 
     def qkv_append_dev(self, model, q, k, v, ctx_lens, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """Device tensors, bf16 [B][heads][D] (views of a fused projection will do), int32 [B]; only enqueues.  Rows beyond B are not looked at;
