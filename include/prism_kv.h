@@ -143,8 +143,8 @@ int model_register_ex(int pool, int q_heads, int kv_heads, int head_dim, int dty
  * model, the e4m3 header included); block ids, slots, the block table and every bookkeeping
  * call are shared by the layers, frames hold frame_bytes / (n_layers * layer bytes) blocks
  * (PKV_E_SHAPE if that is zero).  pkv_set_layer picks the layer (0 at registration) that
- * kv_write, kv_append, kv_append_chunk, kv_read, decode_attention, decode_attention_multi
- * and prefill_attention address from then on; it is host state only (no device work,
+ * kv_write, kv_append, kv_append_chunk, qkv_append, qkv_append_chunk, kv_read, kv_gather and the
+ * calls of decode and prefill attention address from then on; it is host state only (no device work,
  * PKV_E_ARG outside 0..n_layers-1) and takes effect for calls enqueued after it. */
 int model_register_layers(int pool, int q_heads, int kv_heads, int head_dim, int dtype,
                           int max_seqs, int max_blocks_per_seq, int n_layers);
@@ -398,8 +398,9 @@ int prefill_attention(int model, int batch, const void *q, const int32_t *q_lens
  * time, nor one with a decode_attention* call.  Otherwise they only enqueue.
  *
  * decode_attention_prefix: q dev bf16 [batch][q_heads][head_dim], out [batch][q_heads][head_dim].  Sequences
- * with the same prefix_seqs and prefix_blocks form a group; a group's prefix is read once for all its members,
- * in any order of the batch.
+ * with the same prefix_seqs and prefix_blocks form a group, in any order of the batch; a group's prefix is walked for 128
+ * columns (members x heads of a kv head) at a time, not for each member, except in small calls, where every sequence walks its
+ * prefix for itself in one launch.
  * prefill_attention_prefix: query i of sequence s stands behind the prefix and ctx_lens[s] - q_lens[s] + i
  * tokens of its own and sees all of those and itself; one that would stand before its row's first token
  * (ctx_lens[s] below q_lens[s]) sees the prefix alone, as a decode step with a context length of 0 does. */

@@ -406,7 +406,8 @@ __device__ __forceinline__ void turn_queries(const AttnDesc &d, const QkvArgs &a
 }
 
 // The decode step.  One wave per (sequence, kv head) for K and V of its new token, the element layout of k_kv_append, then
-// waves for the queries.  Bound by dependent memory trips (context length, block id, the block).
+// waves for the queries.  Bound by dependent memory trips (context length, block id, the block): 64 rows of 32/8/128 4.0 us, into an e4m3 cache
+// 5.3, and 19.9 where every token raises its blocks' scales (the codes of earlier slots go one slot after the other).
 template <int DT>
 __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvArgs a) {
     const int lane = threadIdx.x, D = d.D, kv_waves = d.batch * d.Hkv;
@@ -478,7 +479,8 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
 }
 
 // Bound by memory: ragged prompts of 4300 tokens of 32/8/128, neighbours as pairs, 115 MB, cold: 26.1 us (22.6 at a large copy's rate).  39.0 with every head's weights and angles looked up and worked out by themselves, one row in flight a wave;
-// with registers for five waves a SIMD instead of four 32.4, for three 28.9.  2400 tokens into an e4m3 cache 14.5 (before 23.5).
+// 96 registers, five waves a SIMD; with 80, six, some 200 to 350 spill (bf16 26.0, e4m3 with its way back 23.9 instead of 19.5).
+// 2400 tokens into an e4m3 cache 15.9 (first kernel 23.5), 4.9 million vector instructions, some 9 us of issue, beside 46 MB.
 // With V read in pieces of 8 bytes 26.5.
 // A prefill chunk.  Waves of whole pages as in k_kv_append_chunk (one per page that the chunk touches, kv head, and K or V), then waves for
 // the queries, each with some heads of one token.  (Queries first: the prompts above 29.6 us, 27.5 so; 2000 tokens into an e4m3 cache, with their way
