@@ -409,6 +409,46 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
 int prefill_attention_prefix(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *prefix_seqs,
                              const int32_t *prefix_blocks, const int32_t *ctx_lens, float *out);
 
+/* ---- windows with sinks, and drafted trees ------------------------------------
+ * Layers whose queries do not see all that is cached, and drafted tokens that are verified many at a time.  Everything not said
+ * here is as in decode_attention_ex (with the library's table), prefill_attention and qkv_append_chunk: outputs dev fp32, fp32 accumulation, 16
+ * significant bits of every probability on both cache types, zero rows where nothing is seen.  What a query does not see does
+ * not reach it, whatever it holds, where none of the call's queries sees it.  Small calls keep partial sums in the split-K workspace, others in a
+ * buffer of the model, made or enlarged when first needed (PKV_E_NOMEM while the stream is being captured: make the call once
+ * before the capture): two of the attention calls of this section on one model must not overlap in time, nor one with a decode_attention* call
+ * or a call behind shared prefixes.  Otherwise they only enqueue.
+ *
+ * A window: the query at position p of its row sees token t <= p if t > p - window or t < sinks: the last `window` tokens, its own
+ * among them, and the first `sinks`.  window >= 1, sinks >= 0 (PKV_E_ARG).  Tokens between are not read.
+ *   decode_attention_window    the query of sequence s stands at position ctx_lens[s] - 1
+ *   prefill_attention_window   query i of sequence s at position ctx_lens[s] - q_lens[s] + i
+ *
+ * A drafted tree: the last q_lens[s] of the ctx_lens[s] tokens of a row are drafted ones, in any order in which a token comes behind those that
+ * it continues; ctx_lens[s] - q_lens[s] = base tokens are in front of them.
+ *   sees   dev uint64 [sum q_lens][words], 8-byte aligned, words 1 .. 4: bit j & 63 of word j >> 6 of a drafted token's row says whether it sees
+ *          drafted token j of its sequence; itself has to be said too.  Bits from q_lens[s] on are not looked at.  A
+ *          token that sees n >= 1 drafted ones stands at position base + n - 1 (none: base).
+ * PKV_E_RANGE where q_lens[s] > 64 * words.  A chain is the tree whose token i sees drafted tokens 0 .. i.
+ *   qkv_append_tree   qkv_append_chunk with those positions (and before[s] in front of them) in the rotation
+ *   tree_attention    drafted token i sees the tokens in front of the drafts, with window >= 1 those of its position's window and the sinks
+ *                     (0: all; a window below q_lens[s] is refused, PKV_E_ARG), and the drafted ones of its row of `sees`.  A row whose context
+ *                     length is below its q_lens gives zeros.
+ *   kv_keep           drafted tokens kept[0] < kept[1] < ... of sequence s (its n_kept[s] first entries of the q_lens[s] that it has in
+ *                     `kept`, dev int32 [sum q_lens]) are moved to base, base + 1, ..., in all layers of the model; n_kept: dev
+ *                     int32 [batch].  new_lens: dev int32 [batch] or NULL, apart from the others (PKV_E_ARG): receives base + n_kept[s].
+ *                     Tokens behind those hold whatever they held or worse; blocks stay reserved.  bf16: values as they
+ *                     were.  e4m3: a token that is in its place already (kept[j] = j, as all in front of it) keeps its
+ *                     code; the others are what kv_gather gives of them, appended one by one by the rule of kv_append.  A
+ *                     row whose entries are not ascending and within 0 .. q_lens[s] - 1, or whose context length does not fit, is left
+ *                     as it is and raises bit 1 of pkv_device_errors(); its new_lens is ctx_lens[s].  Returns batch; only enqueues. */
+int decode_attention_window(int model, int batch, const void *q, const int32_t *ctx_lens, int window, int sinks, float *out);
+int prefill_attention_window(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, int window, int sinks, float *out);
+int qkv_append_tree(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words,
+                    void *q_out);
+int tree_attention(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words, int window,
+                   int sinks, float *out);
+int kv_keep(int model, int batch, const int32_t *q_lens, const int32_t *ctx_lens, const int32_t *kept, const int32_t *n_kept, int32_t *new_lens);
+
 /* ---- observation ----------------------------------------------------------- */
 
 /* Canonical image of the bookkeeping state as little-endian int32 words:

@@ -84,6 +84,11 @@ def _load():
         "decode_attention_prefix": (i, [i, i, vp, vp, vp, vp, vp]),
         "prefill_attention_prefix": (i, [i, i, vp, vp, vp, vp, vp, vp]),
         "kv_gather": (i, [i, i, vp, vp, vp, vp, vp]),
+        "decode_attention_window": (i, [i, i, vp, vp, i, i, vp]),
+        "prefill_attention_window": (i, [i, i, vp, vp, vp, i, i, vp]),
+        "qkv_append_tree": (i, [i, i, vp, vp, vp, vp, i, vp]),
+        "tree_attention": (i, [i, i, vp, vp, vp, vp, i, i, i, vp]),
+        "kv_keep": (i, [i, i, vp, vp, vp, vp, vp]),
         "rotary_frequencies": (i, [i, C.c_double, i, C.c_double, C.c_double, C.c_double, C.c_double, vp]),
         "rotary_create": (i, [i, i, vp, C.c_double]),
         "rotary_destroy": (i, [i]),
@@ -119,7 +124,8 @@ EXPORTS = ["pkv_set_stream", "pkv_last_error", "pkv_device_errors", "pkv_set_spl
            "pkv_ticket_result", "model_block_table", "kv_write", "kv_append", "kv_append_chunk", "kv_read", "model_set_batch", "decode_attention",
            "decode_attention_ex", "decode_attention_static", "decode_attention_multi", "prefill_attention", "pool_export_state", "pool_stats",
            "arbitrate_requests", "place_models", "rotary_frequencies", "rotary_create", "rotary_destroy", "qkv_append", "qkv_append_chunk",
-           "kv_gather", "decode_attention_prefix", "prefill_attention_prefix"]
+           "kv_gather", "decode_attention_prefix", "prefill_attention_prefix",
+           "decode_attention_window", "prefill_attention_window", "qkv_append_tree", "tree_attention", "kv_keep"]
 
 
 # Calls of few tokens take the host longer than the GPU: their addresses go as plain integers and their host lists as bytes, not as c_void_p and numpy
@@ -132,6 +138,11 @@ def _at(tensor):
 def _i32(a):
     """A host int32 list or array as the bytes that a call reads."""
     return np.asarray(a, dtype=np.int32).tobytes()
+
+
+def _total(lens):
+    """Sum of a host list as _i32 makes it."""
+    return sum(memoryview(lens).cast("i")) if len(lens) <= 256 else int(np.frombuffer(lens, dtype=np.int32).sum(dtype=np.int64))
 
 
 def _f64(a):
@@ -482,8 +493,7 @@ class PrismKV:
         """The same for packed chunks; q_lens: list or host int32 array.  Only enqueues."""
         ql = _i32(q_lens)
         n = len(ql) // 4
-        tokens = sum(memoryview(ql).cast("i")) if n <= 64 else int(np.frombuffer(ql, dtype=np.int32).sum(dtype=np.int64))
-        x = self._qkv(model, n, tokens, q_out, q, k, v, q_weight, k_weight, eps, rotary, before) if ctx_lens.numel() >= n else None
+        x = self._qkv(model, n, _total(ql), q_out, q, k, v, q_weight, k_weight, eps, rotary, before) if ctx_lens.numel() >= n else None
         return self.lib.qkv_append_chunk(model, n, x, ql, ctx_lens.data_ptr(), q_out.data_ptr() if x else None)
 
     def kv_read(self, model, seq, tok_begin, n_tok):
@@ -561,6 +571,45 @@ class PrismKV:
         ql, ps, pb, n = _i32(q_lens), _i32(prefix_seqs), _i32(prefix_blocks), ctx_lens.numel()
         assert len(ql) == len(ps) == len(pb) == 4 * n
         return self.lib.prefill_attention_prefix(model, n, _at(q), ql, ps, pb, _at(ctx_lens), _at(out))
+
+    # ---- windows with sinks, and drafted trees
+    def decode_attention_window_dev(self, model, q, ctx_lens, window, sinks, out):
+        """q, ctx_lens, out: device tensors.  Only enqueues."""
+        return self.lib.decode_attention_window(model, ctx_lens.numel(), _at(q), _at(ctx_lens), window, sinks, _at(out))
+
+    def prefill_attention_window_dev(self, model, q, q_lens, ctx_lens, window, sinks, out):
+        """The same for packed chunks; q_lens: list or host int32 array.  Only enqueues."""
+        ql, n = _i32(q_lens), ctx_lens.numel()
+        assert len(ql) == 4 * n
+        return self.lib.prefill_attention_window(model, n, _at(q), ql, _at(ctx_lens), window, sinks, _at(out))
+
+    def _tree(self, ql, ctx_lens, sees):
+        """Words of a row of a tree's mask; 0, which the library refuses, where a tensor holds less than the call would read."""
+        tokens = _total(ql)
+        if sees.element_size() != 8 or sees.dim() != 2 or not sees.is_contiguous() or sees.shape[0] < tokens or 4 * ctx_lens.numel() < len(ql):
+            return 0
+        return sees.shape[1]
+
+    def qkv_append_tree_dev(self, model, q, k, v, q_lens, ctx_lens, sees, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
+        """qkv_append_chunk_dev of drafted tokens; sees: device tensor, int64 (bits) [tokens][words].  Only enqueues."""
+        ql = _i32(q_lens)
+        n, words = len(ql) // 4, self._tree(ql, ctx_lens, sees)
+        x = self._qkv(model, n, _total(ql), q_out, q, k, v, q_weight, k_weight, eps, rotary, before)
+        return self.lib.qkv_append_tree(model, n, x, ql, _at(ctx_lens), _at(sees), words, q_out.data_ptr() if x else None)
+
+    def tree_attention_dev(self, model, q, q_lens, ctx_lens, sees, out, window=0, sinks=0):
+        """Drafted tokens over their contexts; sees as in qkv_append_tree_dev.  Only enqueues."""
+        ql = _i32(q_lens)
+        return self.lib.tree_attention(model, len(ql) // 4, _at(q), ql, _at(ctx_lens), _at(sees), self._tree(ql, ctx_lens, sees), window, sinks, _at(out))
+
+    def kv_keep_dev(self, model, q_lens, ctx_lens, kept, n_kept, new_lens=None):
+        """Device tensors, int32: kept [tokens], n_kept and new_lens [B]; q_lens: list or host int32 array.  All layers; only enqueues."""
+        ql = _i32(q_lens)
+        n = len(ql) // 4
+        tokens = _total(ql)
+        fits = kept.nbytes >= 4 * tokens and n_kept.nbytes >= 4 * n and ctx_lens.nbytes >= 4 * n and (new_lens is None or new_lens.nbytes >= 4 * n)
+        fits = fits and all(x is None or x.is_contiguous() for x in (kept, n_kept, ctx_lens, new_lens))
+        return self.lib.kv_keep(model, n, ql, _at(ctx_lens), _at(kept) if fits else None, _at(n_kept), _at(new_lens))
 
     def prefill_attention(self, model, q, q_lens, ctx_lens):
         """Convenience for tests: -> (code, out as numpy fp32 [sum q_lens][Hq][D])."""

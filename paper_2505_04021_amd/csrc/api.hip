@@ -1935,7 +1935,19 @@ int qkv_append(int model, int batch, const pkv_qkv *in, const int32_t *ctx_lens,
     return batch;
 }
 
-int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, void *q_out) {
+// What calls of drafted trees are given of their masks.
+static int check_tree(int batch, const int32_t *q_lens, const uint64_t *sees, int words, int window) {
+    if (!sees || ((uintptr_t)sees & 7) || words < 1 || words > PKV_TREE_WORDS) return PKV_E_ARG;
+    for (int s = 0; s < batch; ++s) {
+        if (q_lens[s] > 64 * words) return PKV_E_RANGE;
+        if (window > 0 && q_lens[s] > window) return PKV_E_ARG;
+    }
+    return PKV_OK;
+}
+
+// qkv_append_chunk, and with `tree` qkv_append_tree.
+static int run_qkv_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words, bool tree,
+                         void *q_out) {
     Model *m = get_model(model);
     if (!m) return PKV_E_HANDLE;
     if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
@@ -1950,8 +1962,13 @@ int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_l
     if (total == 0) return 0;
     if (!in) return PKV_E_ARG;
     QkvArgs a{};
-    const int rc = fill_qkv(a, *m, *in, q_out);
+    int rc = fill_qkv(a, *m, *in, q_out);
+    if (!rc && tree) rc = check_tree(batch, q_lens, sees, words, 0);
     if (rc) return rc;
+    if (tree) {
+        a.sees = sees;
+        a.words = words;
+    }
     a.wave_heads = wave_heads_for(*m, total);
     AttnDesc d{};
     fill_addressing(d, *m);
@@ -1967,6 +1984,15 @@ int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_l
     }
     HIP_TRY(pkv_launch_qkv_append_chunk(d, a, plan.take(batch), g_stream));
     return (int)total;
+}
+
+int qkv_append_chunk(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, void *q_out) {
+    return run_qkv_chunk(model, batch, in, q_lens, ctx_lens, nullptr, 0, false, q_out);
+}
+
+int qkv_append_tree(int model, int batch, const pkv_qkv *in, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words,
+                    void *q_out) {
+    return run_qkv_chunk(model, batch, in, q_lens, ctx_lens, sees, words, true, q_out);
 }
 
 int model_set_batch(int model, int batch, int row_stride) {
@@ -2447,6 +2473,151 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
         HIP_TRY(pkv_launch_prefix(d, plan, g_stream));
     }
     return PKV_OK;
+}
+
+/* ------------------------------------------------ windows and drafted trees */
+
+// Pages that the last query of a sequence walks, as far as the host knows.
+static int masked_pages(int pages, int window, int sinks, int queries) {
+    const int64_t most = (int64_t)(sinks + 15) / 16 + ((int64_t)window + queries + 15) / 16 + 1;
+    return pages < most ? pages : (int)most;
+}
+
+static void masked_desc(AttnDesc &d, const Model &m, int batch, const void *q, const int32_t *ctx_lens, float *out) {
+    fill_addressing(d, m);
+    d.q = (const uint16_t *)q;
+    d.ctx_lens = ctx_lens;
+    d.out = out;
+    d.batch = batch;
+    d.cols = m.g;
+    d.scale_log2 = (float)(1.4426950408889634 / sqrt((double)m.D));
+    d.ws = m.ws;
+    d.cnt = m.cnt;
+}
+
+// Pages of a part where `units` work-groups would walk up to `longest` pages uncut.
+static int masked_part_pages(int64_t units, int longest, int64_t most_units) {
+    int64_t parts = units > 0 ? kSmallWorkGroups / units : 1;
+    if (parts > longest / kSmallPart[0]) parts = longest / kSmallPart[0];
+    if (parts > kSmallMaxParts) parts = kSmallMaxParts;
+    while (parts > 1 && units * parts > most_units) --parts;
+    if (parts < 1) parts = 1;
+    int size = (int)((longest + parts - 1) / parts + 7) / 8 * 8;
+    return size < 8 ? 8 : size;
+}
+
+static MaskArgs mask_args(int window, int sinks) {
+    MaskArgs mk{};
+    mk.window = window > 0 && window < PKV_NO_WINDOW ? window : PKV_NO_WINDOW;
+    mk.sinks = sinks < PKV_NO_WINDOW ? sinks : PKV_NO_WINDOW;
+    return mk;
+}
+
+int decode_attention_window(int model, int batch, const void *q, const int32_t *ctx_lens, int window, int sinks, float *out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0) return PKV_E_ARG;
+    if (batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return PKV_OK;
+    if (!q || !ctx_lens || !out || window < 1 || sinks < 0) return PKV_E_ARG;
+    if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return PKV_E_ARG;
+    AttnDesc d{};
+    masked_desc(d, *m, batch, q, ctx_lens, out);
+    const MaskArgs mk = mask_args(window, sinks);
+    int longest = 1;
+    for (int s = 0; s < batch; ++s) {
+        const int pages = masked_pages(m->row_len[s], mk.window, mk.sinks, 1);
+        longest = longest > pages ? longest : pages;
+    }
+    d.part_pages = masked_part_pages((int64_t)batch * m->Hkv, longest, (int64_t)(m->ws_floats / partial_floats(m->g, m->D)));
+    d.parts = (longest + d.part_pages - 1) / d.part_pages;
+    HIP_TRY(pkv_launch_window(d, mk, g_stream));
+    return PKV_OK;
+}
+
+// prefill_attention_window, and with `tree` tree_attention.
+static int run_masked(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words, bool tree,
+                      int window, int sinks, float *out) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return PKV_OK;
+    if (!q || !q_lens || !ctx_lens || !out || window < (tree ? 0 : 1) || sinks < 0) return PKV_E_ARG;
+    if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return PKV_E_ARG;
+    int64_t total = 0;
+    for (int s = 0; s < batch; ++s) {
+        if (q_lens[s] < 0) return PKV_E_ARG;
+        total += q_lens[s];
+        if (total > (int64_t)1 << 24) return PKV_E_RANGE;
+    }
+    if (tree) {
+        const int rc = check_tree(batch, q_lens, sees, words, window);
+        if (rc) return rc;
+    }
+    if (total == 0) return PKV_OK;
+    AttnDesc d{};
+    masked_desc(d, *m, batch, q, ctx_lens, out);
+    MaskArgs mk = mask_args(window, sinks);
+    mk.sees = sees;
+    mk.words = words;
+    const int group = 16 / m->g;
+    int64_t groups = 0;
+    int longest = 1;
+    for (int s = 0; s < batch; ++s) {
+        groups += (q_lens[s] + group - 1) / group;
+        const int pages = q_lens[s] ? masked_pages(m->row_len[s], mk.window, mk.sinks, group) : 0;
+        longest = longest > pages ? longest : pages;
+    }
+    if (groups * kSmallMaxParts >= 1 << 22) return PKV_E_RANGE;
+    const int64_t slots = (int64_t)(m->ws_floats / partial_floats(16, m->D));
+    d.part_pages = masked_part_pages(groups * m->Hkv, longest, slots < (int64_t)m->cnt_cap ? slots : (int64_t)m->cnt_cap);
+    PlanBuilder plan(batch);
+    for (int s = 0; s < batch; ++s) {
+        if (plan.full()) HIP_TRY(pkv_launch_masked(d, mk, plan.take(s), tree, g_stream));
+        const int pages = masked_pages(m->row_len[s], mk.window, mk.sinks, group), n = (q_lens[s] + group - 1) / group;
+        const int parts = pages > d.part_pages ? (pages + d.part_pages - 1) / d.part_pages : 1;
+        plan.add((uint32_t)q_lens[s], (uint32_t)(n * parts), (uint32_t)parts, (uint32_t)(pages / parts));
+    }
+    HIP_TRY(pkv_launch_masked(d, mk, plan.take(batch), tree, g_stream));
+    return PKV_OK;
+}
+
+int prefill_attention_window(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, int window, int sinks, float *out) {
+    return run_masked(model, batch, q, q_lens, ctx_lens, nullptr, 0, false, window, sinks, out);
+}
+
+int tree_attention(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, const uint64_t *sees, int words, int window,
+                   int sinks, float *out) {
+    return run_masked(model, batch, q, q_lens, ctx_lens, sees, words, true, window, sinks, out);
+}
+
+int kv_keep(int model, int batch, const int32_t *q_lens, const int32_t *ctx_lens, const int32_t *kept, const int32_t *n_kept, int32_t *new_lens) {
+    Model *m = get_model(model);
+    if (!m) return PKV_E_HANDLE;
+    if (batch < 0 || batch > m->dev.max_seqs) return PKV_E_RANGE;
+    if (batch == 0) return 0;
+    if (!q_lens || !ctx_lens || !kept || !n_kept) return PKV_E_ARG;
+    int64_t total = 0;
+    for (int s = 0; s < batch; ++s) {
+        if (q_lens[s] < 0) return PKV_E_ARG;
+        total += q_lens[s];
+        if (total > (int64_t)1 << 24) return PKV_E_RANGE;
+    }
+    // (what all work-groups of a row read is not written by one of them)
+    auto apart = [&](const int32_t *x, int64_t n) { return new_lens + batch <= x || x + n <= new_lens; };
+    if (new_lens && !(apart(ctx_lens, batch) && apart(n_kept, batch) && apart(kept, total))) return PKV_E_ARG;
+    AttnDesc d{};
+    fill_addressing(d, *m);
+    d.pool_base = g_pools[m->pool].base;                 // layer 0
+    d.batch = batch;
+    d.ctx_lens = ctx_lens;
+    PlanBuilder plan(batch);
+    for (int s = 0; s < batch; ++s) {
+        if (plan.full()) HIP_TRY(pkv_launch_kv_keep(d, plan.take(s), m->L, m->layer_bytes, kept, n_kept, new_lens, g_stream));
+        plan.add((uint32_t)q_lens[s], 0u, 0u, 0u);
+    }
+    HIP_TRY(pkv_launch_kv_keep(d, plan.take(batch), m->L, m->layer_bytes, kept, n_kept, new_lens, g_stream));
+    return batch;
 }
 
 int decode_attention(int model, const void *q, const int32_t *block_table, const int32_t *ctx_lens, float *out) {

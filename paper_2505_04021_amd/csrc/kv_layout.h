@@ -113,3 +113,14 @@ struct PlanLanes {
         return r;
     }
 };
+
+// How many drafted tokens a token sees by its row of a tree's mask, of the first `n`.
+__device__ __forceinline__ int seen_drafts(const uint64_t *row, int words, int n) {
+    int count = 0;
+    for (int i = 0; i < words; ++i) {
+        const int left = n - 64 * i;
+        const uint64_t some = left >= 64 ? ~0ull : (left <= 0 ? 0ull : (1ull << left) - 1ull);
+        count += __popcll(row[i] & some);
+    }
+    return count;
+}

@@ -350,34 +350,16 @@ __device__ __forceinline__ uint32_t lower_codes(uint32_t w, uint32_t lo, uint32_
 // on the border of two codes, as two of three waves hold some); 10.0 so (517).
 constexpr int FEW_LANES = 4;
 
-template <int D, bool IS_V, typename TILE_OF, typename TURN>
-__device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const PageRows &p, TURN &&turn) {
+// Values of slots s0 .. end - 1 into a tile: x as TURN leaves it, two per word; K: elements of units (i, c), 8 (8 i + c) .. + 7 and 8 (8 i + 4 + c) .. + 7;
+// V: elements 64 i + 16 u + 4 c .. + 3.  ready(): makes them so once the block is known.
+template <int D, bool IS_V, typename TILE_OF, typename READY>
+__device__ __forceinline__ void quantise_values(uint32_t *x, const TILE_OF &tile_of, const int s0, const int end, READY &&ready) {
     constexpr int NW = D / 16;                           // words of codes per lane
     const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4, G = t >> 2, e = t & 3;
-    const int s0 = p.s0, end = p.s0 + p.n;
-    uint32_t x[2 * NW];                                  // this lane's values, two per word
-    read_rows(p, [&](auto a) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            if constexpr (!IS_V) {                       // elements of units (i, c): 8 (8 i + c) .. + 7 and 8 (8 i + 4 + c) .. + 7
-                row_bytes<16, 2, decltype(a)::value>(x + 8 * i, p, t, 16 * (8 * i + c));
-                row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 4, p, t, 16 * (8 * i + 4 + c));
-            } else {                                     // elements 64 i + 16 u + 4 c .. + 3
-#pragma unroll
-                for (int u = 0; u < 4; u += 2) row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 2 * u, p, t, 2 * (64 * i + 16 * u + pair_piece(c)));
-            }
-        }
-    });
-    if constexpr (!IS_V) turn.ask(p, t, c);
-    asked_for();
     float *scale_p;
     uint8_t *tile = tile_of(scale_p);
     if (!tile) return;
-    if constexpr (!IS_V) turn.turn(x);
-    else {
-#pragma unroll
-        for (int i = 0; i < NW / 2; ++i) exchange_pair(x + 4 * i);
-    }
+    ready();
     // what the tile holds: codes of the slots before
     u32x4 old[D / 64];
     u32x4 *unit = reinterpret_cast<u32x4 *>(tile + (IS_V ? (G * 16 + 4 * c + e) * 16 : (c * 16 + t) * 16));
@@ -543,6 +525,34 @@ __device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const Page
             put_v_unit<1>(reinterpret_cast<uint8_t *>(unit + 64 * i), v, G, first, end);
         }
     }
+}
+
+template <int D, bool IS_V, typename TILE_OF, typename TURN>
+__device__ __forceinline__ void page_quantise(const TILE_OF &tile_of, const PageRows &p, TURN &&turn) {
+    constexpr int NW = D / 16;                           // words of codes per lane
+    const int lane = threadIdx.x & 63, t = lane & 15, c = lane >> 4;
+    uint32_t x[2 * NW];                                  // this lane's values, two per word
+    read_rows(p, [&](auto a) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            if constexpr (!IS_V) {                       // elements of units (i, c): 8 (8 i + c) .. + 7 and 8 (8 i + 4 + c) .. + 7
+                row_bytes<16, 2, decltype(a)::value>(x + 8 * i, p, t, 16 * (8 * i + c));
+                row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 4, p, t, 16 * (8 * i + 4 + c));
+            } else {                                     // elements 64 i + 16 u + 4 c .. + 3
+#pragma unroll
+                for (int u = 0; u < 4; u += 2) row_bytes<16, 2, decltype(a)::value>(x + 8 * i + 2 * u, p, t, 2 * (64 * i + 16 * u + pair_piece(c)));
+            }
+        }
+    });
+    if constexpr (!IS_V) turn.ask(p, t, c);
+    asked_for();
+    quantise_values<D, IS_V>(x, tile_of, p.s0, p.s0 + p.n, [&]() __attribute__((always_inline)) {
+        if constexpr (!IS_V) turn.turn(x);
+        else {
+#pragma unroll
+            for (int i = 0; i < NW / 2; ++i) exchange_pair(x + 4 * i);
+        }
+    });
 }
 
 // One wave's share of a page: the K (which = 0) or V (1) tile of kv head h.  QUANT: bf16 values into an e4m3 block.

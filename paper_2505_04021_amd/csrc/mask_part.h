@@ -1,0 +1,348 @@
+// Which tokens a query sees where that is not simply "all up to its own" (gfx950): a sliding window with sinks, or the ancestors of a
+// drafted token behind its context; and the work-group that walks one part of such a context for up to 16 columns.
+//
+//   out = softmax over the seen t of (q . k_t / sqrt D) V
+//
+// A query at position p sees token t <= p where t > p - window or t < sinks.  A drafted token sees the cached tokens in front of the drafts by the
+// same rule, p being the position that its depth gives it, and of the drafted ones those whose bit is set in its row of the mask.
+#pragma once
+#include "decode_part.h"
+
+namespace {
+
+// The tokens that some query of a unit may see, as one walk along pages: the sinks' pages, then those from the first query's window on.
+// Tokens are counted along the walk: those behind the gap are 16 * skip fewer than in the row.
+struct Walk {
+    int len;                 // tokens, to the end of what the last query sees
+    int front, skip;         // pages in front of the gap; pages left out
+    int sinks;               // tokens in front that every query sees
+    int lo_min, lo_max;      // where the windows of the first and of the last query begin
+    int hi_min;              // tokens that all queries see, but for the windows
+    __device__ __forceinline__ int page(int i) const { return i < front ? i : i + skip; }
+    __device__ __forceinline__ int pages() const { return (len + PKV_T - 1) / PKV_T; }
+    // whether every query sees all 32 tokens of pair p
+    __device__ __forceinline__ bool plain(int x0) const { return (x0 + 32 <= hi_min) & ((x0 >= lo_max) | (x0 + 32 <= sinks)); }
+};
+
+// L tokens of the row; windows that begin at token `lo_min` and `lo_max`; all queries see tokens below `hi_min`, as far as windows go
+__device__ __forceinline__ Walk walk_of(int L, int lo_min, int lo_max, int hi_min, int sinks) {
+    Walk w;
+    L = L < 0 ? 0 : L;
+    auto within = [&](int x) __attribute__((always_inline)) { return x < 0 ? 0 : (x < L ? x : L); };
+    w.sinks = within(sinks);
+    lo_min = within(lo_min);
+    w.front = (w.sinks + PKV_T - 1) / PKV_T;
+    const int first = lo_min / PKV_T;
+    w.skip = first > w.front ? first - w.front : 0;
+    const int shift = w.skip * PKV_T;
+    w.len = L - shift;
+    w.lo_min = lo_min - shift;
+    w.lo_max = within(lo_max) - shift;
+    w.hi_min = within(hi_min) - shift;
+    return w;
+}
+
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); }
+
+// A column's 32 tokens from x0 on: seen are those below `hi` that are sinks or not below `lo`
+__device__ __forceinline__ uint32_t seen_bits(int x0, int hi, int lo, int sinks) {
+    return below(hi - x0) & (~below(lo - x0) | below(sinks - x0));
+}
+
+// Rows of a tree's mask in LDS: bits [from, from + 32) of a row of `words` 32-bit words, zeros beyond it
+__device__ __forceinline__ uint32_t row_bits(const uint32_t *row, int words, int from) {
+    const int i = from >> 5;                              // (arithmetic: -1 for the 32 bits in front)
+    auto word = [&](int k) __attribute__((always_inline)) {
+        const uint32_t x = row[k < 0 ? 0 : (k < words ? k : words - 1)];
+        return k >= 0 && k < words ? x : 0u;
+    };
+    return __builtin_amdgcn_alignbit(word(i + 1), word(i), (uint32_t)from & 31u);
+}
+
+// One work-group's part of a launch: up to 16 columns, `tokens` query tokens x the g heads of a kv head.
+struct MaskUnit {
+    int seq, kvh, part, parts, size;     // which of how many parts of the walk, of how many pages
+    int first, tokens;                   // rows of q and out
+    int slot;                            // arrival counter of the unit
+    size_t partial;                      // its partial sums (of part 0; the others follow `step` apart)
+    size_t step;
+    int chunk0, chunk;                   // the first of them among its sequence's, and how many those are
+};
+
+// Blanks the tokens of a V tile that no query sees, which may hold anything (even NaN); a set bit: seen
+template <int D, int DT>
+__device__ __forceinline__ void keep_v(u32x4 *v, uint32_t four) {
+    const uint32_t m01 = (four & 1u ? 0xffffu : 0u) | (four & 2u ? 0xffff0000u : 0u), m23 = (four & 4u ? 0xffffu : 0u) | (four & 8u ? 0xffff0000u : 0u);
+    const uint32_t m = (four & 1u ? 0xffu : 0u) | (four & 2u ? 0xff00u : 0u) | (four & 4u ? 0xff0000u : 0u) | (four & 8u ? 0xff000000u : 0u);       // codes
+#pragma unroll
+    for (int j = 0; j < Tile<D, DT>::NL; ++j) v[j] &= DT == PKV_BF16 ? mk4(m01, m23, m01, m23) : mk4(m, m, m, m);
+}
+
+constexpr int MASK_COLS = 16, MASK_WORDS = 2 * PKV_TREE_WORDS;      // columns of a unit; 32-bit words of a row of a tree's mask
+
+// The work-group's four waves take the page pairs of its part in turn and join their sums through LDS; the last of several parts to arrive joins
+// those through memory (as attn_part in decode_part.h, whose comments say why it is built like this).
+template <int D, int DT, bool TREE>
+__device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &mk, const MaskUnit &u, float *s_acc, float *s_m, float *s_l, uint32_t *s_mask,
+                                            uint32_t *s_arrived) {
+    using TL = Tile<D, DT>;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int G = lane >> 4, n = lane & 15, g = d.g, cols = u.tokens * g;
+    const int32_t *row = d.table + (size_t)u.seq * d.row_stride;
+    const bool col_live = n < cols;
+    const int tok = col_live ? n / g : 0;
+    bf16x8 qf[TL::NK];
+    {
+        const uint16_t *qrow = d.q + ((size_t)(u.first + tok) * d.Hq + u.kvh * g + (col_live ? n - tok * g : 0)) * D;
+#pragma unroll
+        for (int j = 0; j < TL::NK; ++j) {
+            u32x4 v = mk4(0, 0, 0, 0);
+            if (col_live) v = *reinterpret_cast<const u32x4 *>(qrow + 8 * (4 * j + G));
+            qf[j] = *reinterpret_cast<bf16x8 *>(&v);
+        }
+    }
+    int ctx = PKV_CONST(int32_t, d.ctx_lens)[u.seq], cap = PKV_CONST(int32_t, d.row_len)[u.seq];
+    asm volatile("" : "+s"(ctx), "+s"(cap));              // both at once
+    cap *= PKV_T;
+    // what this lane's column sees, in tokens of the row
+    const int window = mk.window;
+    int base = 0, hi, lo, L, lo_first, lo_last, hi_first;
+    uint32_t *mask_row = s_mask + (w * MASK_COLS + tok) * MASK_WORDS;
+    if constexpr (TREE) {
+        base = ctx - u.chunk;
+        L = base < 0 ? 0 : (ctx < cap ? ctx : cap);
+        const uint64_t *bits = mk.sees + (size_t)(u.first + tok) * mk.words;
+        const int seen = seen_drafts(bits, mk.words, u.chunk);
+        for (int i = 0; i < mk.words; ++i) {
+            const uint64_t x = bits[i];
+            mask_row[2 * i] = (uint32_t)x;
+            mask_row[2 * i + 1] = (uint32_t)(x >> 32);
+        }
+        hi = base;
+        lo = base + (seen > 0 ? seen : 1) - window;
+        lo_first = base + 1 - window;
+        lo_last = base + u.chunk - window;
+        hi_first = base;
+    } else {
+        L = ctx < 0 ? 0 : (ctx < cap ? ctx : cap);
+        const int pos0 = L - u.chunk + u.chunk0;          // of the unit's first query
+        L = pos0 + u.tokens;
+        hi = pos0 + tok + 1;
+        lo = hi - window;
+        lo_first = pos0 + 1 - window;
+        lo_last = L - window;
+        hi_first = pos0 + 1;
+    }
+    const Walk walk = walk_of(L, lo_first, lo_last, hi_first, mk.sinks);
+    const int shift = walk.skip * PKV_T;
+    hi -= shift;
+    lo -= shift;
+    base -= shift;
+    const int n_pages = walk.pages(), max_parts = u.parts;
+    constexpr int STEP = 2 * SMALL_WAVES;
+    int size = u.size;
+    if (n_pages > max_parts * size) {                     // longer than the host knew
+        size = (n_pages + max_parts - 1) / max_parts;
+        size = (size + STEP - 1) / STEP * STEP;
+    }
+    const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
+    if (u.part >= n_parts) return;
+    const int page0 = u.part * size + 2 * w, pe = (u.part + 1) * size < n_pages ? (u.part + 1) * size : n_pages;
+    State<D, DT> st;
+#pragma unroll
+    for (int jt = 0; jt < TL::NV; ++jt) st.acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m = -INFINITY;
+    st.l = 0.f;
+
+    // This wave's pairs: pages page0 + STEP k and the one behind it.  Lane i works out where page i & 1 of pair window + (i >> 1) is.
+    bool bad = false;
+    uint32_t addr_lo = 0, addr_hi = 0, records = 0;
+    float page_sk = 0.f, page_sv = 0.f;
+    int pair0 = 0;                                        // the lanes' pages are those of pairs pair0 .. pair0 + 31
+    auto locate = [&](int k) __attribute__((always_inline)) {
+        pair0 = k;
+        const int i = page0 + STEP * (k + (lane >> 1)) + (lane & 1), page = walk.page(i);
+        const uint32_t id = (uint32_t)row[page < d.row_stride ? page : d.row_stride - 1];
+        const bool in_pool = id < d.max_block_id, live = i < pe;
+        bad |= live && !in_pool;
+        const uint8_t *blk = block_ptr(d, id);
+        if (DT == PKV_E4M3) {
+            const float *hdr = reinterpret_cast<const float *>(live && in_pool ? blk : reinterpret_cast<const uint8_t *>(d.safe));
+            page_sk = hdr[u.kvh];
+            page_sv = hdr[d.Hkv + u.kvh];
+            blk += PKV_FP8_HEADER;
+        }
+        blk += (size_t)u.kvh * 2 * TL::TILE_BYTES;
+        addr_lo = (uint32_t)(uintptr_t)blk;
+        addr_hi = (uint32_t)((uintptr_t)blk >> 32);
+        records = live && in_pool ? 2 * TL::TILE_BYTES : 0;
+    };
+    auto lane_of = [&](uint32_t x, int at) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)x, at); };
+    auto tiles = [&](int k, int half) __attribute__((always_inline)) {
+        const int at = 2 * (k - pair0) + half;
+        return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t *>(lane_of(addr_lo, at) | (uint64_t)lane_of(addr_hi, at) << 32), 0,
+                                                 (int)lane_of(records, at), 0x00020000);
+    };
+    const int voff = lane * 16;
+    auto load = [&](u32x4 *r, __amdgpu_buffer_rsrc_t rsrc, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < TL::NL; ++j) r[j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff + j * 1024, at, 2 /* non-temporal */);
+        asm volatile("" ::: "memory");                    // in this order everywhere: loads in flight are counted
+    };
+    auto load_pair = [&](PairRegs<D, DT> &r, int k) __attribute__((always_inline)) {
+        const __amdgpu_buffer_rsrc_t a = tiles(k, 0), b = tiles(k, 1);
+        load(r.a.k, a, 0);
+        load(r.a.v, a, TL::TILE_BYTES);
+        load(r.b.k, b, 0);
+        load(r.b.v, b, TL::TILE_BYTES);
+        if (DT == PKV_E4M3) {
+            const int at = 2 * (k - pair0);
+            r.a.sk = __uint_as_float(lane_of(__float_as_uint(page_sk), at));
+            r.a.sv = __uint_as_float(lane_of(__float_as_uint(page_sv), at));
+            r.b.sk = __uint_as_float(lane_of(__float_as_uint(page_sk), at + 1));
+            r.b.sv = __uint_as_float(lane_of(__float_as_uint(page_sv), at + 1));
+        }
+    };
+    auto step = [&](PairRegs<D, DT> &r, PairRegs<D, DT> &o, int k, bool more) __attribute__((always_inline)) {
+        if (more) load_pair(o, k + 1);
+        const int p = page0 + STEP * k, x0 = PKV_T * p;
+        // (Decided ahead of the products, and without branches: the compiler waits for a product's result along one of two ways that part behind it and
+        // meet where it is read, and not along the other.)
+        const bool second = p + 1 < pe, masked = !walk.plain(x0) | !second;
+        const float sca = DT == PKV_E4M3 ? d.scale_log2 * r.a.sk : d.scale_log2, scb = DT == PKV_E4M3 ? d.scale_log2 * r.b.sk : d.scale_log2;
+        const f32x4 sa = qk_page<D, DT>(r.a, qf), sb = qk_page<D, DT>(r.b, qf);
+        float s[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[i] = sa[i] * sca;
+            s[4 + i] = sb[i] * scb;
+        }
+        // pairs with tokens that not every column sees: a branch of its own
+        if (masked) {
+            const uint32_t there = below(walk.len - x0) & (second ? 0xffffffffu : 0xffffu);
+            uint32_t mine = seen_bits(x0, hi, lo, walk.sinks);
+            if constexpr (TREE) mine |= row_bits(mask_row, 2 * mk.words, x0 - base);
+            mine = (mine & there) >> (4 * G);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                  // (a select, so that a NaN logit of an unseen token cannot leak)
+                if (!(mine >> i & 1u)) s[i] = -INFINITY;
+                if (!(mine >> (16 + i) & 1u)) s[4 + i] = -INFINITY;
+            }
+            const uint32_t any = (there & seen_bits(x0, walk.len, walk.lo_min, walk.sinks)) >> (4 * G);
+            keep_v<D, DT>(r.a.v, any);
+            keep_v<D, DT>(r.b.v, any >> 16);
+        }
+        bf16x8 phv, plv;
+        softmax_pair<D, DT>(st, s, r.a.sv, r.b.sv, phv, plv);
+#pragma unroll
+        for (int jt = 0; jt < TL::NV; ++jt) {
+            const u32x2 va = v_half<D, DT>(r.a, jt), vb = v_half<D, DT>(r.b, jt);
+            const bf16x8 av = as_bf16x8(mk4(va.x, va.y, vb.x, vb.y));
+            st.acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, phv, st.acc[jt], 0, 0, 0);
+            st.acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, plv, st.acc[jt], 0, 0, 0);
+        }
+    };
+    const int n_pairs = page0 < pe ? (pe - page0 + STEP - 1) / STEP : 0;
+    if (n_pairs > 0) {
+        PairRegs<D, DT> ring[2];
+        locate(0);
+        load_pair(ring[0], 0);
+        int k = 0;
+        if (n_pairs > 1) {
+            do {
+                if (k + 2 - pair0 >= 32) locate(k + 1);
+                step(ring[0], ring[1], k, true);
+                step(ring[1], ring[0], k + 1, true);
+                k += 2;
+            } while (k + 2 <= n_pairs);
+        }
+        if (k < n_pairs) step(ring[0], ring[1], k, false);
+    }
+    float l = st.l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (n < cols) {
+        float *a = s_acc + (w * cols + n) * D;
+#pragma unroll
+        for (int jt = 0; jt < TL::NV; ++jt) *reinterpret_cast<f32x4 *>(a + 16 * jt + 4 * G) = st.acc[jt];
+        if (G == 0) {
+            s_m[w * 16 + n] = st.m;
+            s_l[w * 16 + n] = l;
+        }
+    }
+    if (__any(bad) && lane == 0) atomicOr(d.err, 1u);
+    __syncthreads();
+    // the sums of the work-group: lane by lane four output elements of one column
+    const int quads = cols * (D / 4);
+    const bool whole = n_parts == 1;
+    float *mine = d.ws + u.partial + u.part * u.step;
+    float *out = d.out + ((size_t)u.first * d.Hq + u.kvh * g) * D;
+    for (int i = threadIdx.x; i < quads; i += 64 * SMALL_WAVES) {
+        const int c = i / (D / 4), x = i - c * (D / 4), t = c / g;
+        float M = s_m[c];
+#pragma unroll
+        for (int v = 1; v < SMALL_WAVES; ++v) M = fmaxf(M, s_m[v * 16 + c]);
+        float den = 0.f;
+        f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < SMALL_WAVES; ++v) {
+            const float f = merge_weight(s_m[v * 16 + c], M);
+            den += f * s_l[v * 16 + c];
+            num += f * *reinterpret_cast<const f32x4 *>(s_acc + (v * cols + c) * D + 4 * x);
+        }
+        if (whole) {
+            *reinterpret_cast<f32x4 *>(out + ((size_t)t * d.Hq + c - t * g) * D + 4 * x) = den != 0.f ? num * (1.0f / den) : num;
+        } else {
+            *reinterpret_cast<f32x4 *>(mine + c * D + 4 * x) = num;
+            if (x == 0) {
+                mine[cols * D + c] = M;
+                mine[cols * D + cols + c] = den;
+            }
+        }
+    }
+    if (whole) return;
+    // partials and counters are in uncached memory: the order of a wave's own accesses is all there is to enforce
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) *s_arrived = atomicAdd(d.cnt + u.slot, 1u);
+    __syncthreads();
+    if (*s_arrived != (uint32_t)(n_parts - 1)) return;
+    if (threadIdx.x == 0) d.cnt[u.slot] = 0u;             // ready for the next launch
+    const float *first = d.ws + u.partial;
+    auto part_sums = [&](f32x4 *v, int c0, int c, int x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = *reinterpret_cast<const f32x4 *>(first + (size_t)(c0 + k < n_parts ? c0 + k : n_parts - 1) * u.step + c * D + 4 * x);
+    };
+    f32x4 v[8];
+    {
+        const int i = (int)threadIdx.x < quads ? (int)threadIdx.x : quads - 1, c = i / (D / 4);
+        part_sums(v, 0, c, i - c * (D / 4));
+    }
+    for (int i = threadIdx.x; i < n_parts * cols; i += 64 * SMALL_WAVES) {
+        const int p = i / cols, c = i - p * cols;
+        s_acc[i] = first[(size_t)p * u.step + cols * D + c];
+        s_acc[MAX_PIECES * 16 + i] = first[(size_t)p * u.step + cols * D + cols + c];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < quads; i += 64 * SMALL_WAVES) {
+        const int c = i / (D / 4), x = i - c * (D / 4), t = c / g;
+        float M = -INFINITY, den = 0.f;
+        f32x4 num = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < n_parts; ++p) M = fmaxf(M, s_acc[p * cols + c]);
+        for (int p0 = 0; p0 < n_parts; p0 += 8) {
+            if (p0 > 0 || i >= 64 * SMALL_WAVES) part_sums(v, p0, c, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (p0 + k < n_parts) {
+                    const float f = merge_weight(s_acc[(p0 + k) * cols + c], M);
+                    den += f * s_acc[MAX_PIECES * 16 + (p0 + k) * cols + c];
+                    num += f * v[k];
+                }
+        }
+        *reinterpret_cast<f32x4 *>(out + ((size_t)t * d.Hq + c - t * g) * D + 4 * x) = den != 0.f ? num * (1.0f / den) : num;
+    }
+}
+
+}  // namespace

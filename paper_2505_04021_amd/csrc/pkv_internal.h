@@ -160,8 +160,19 @@ struct QkvArgs {
     int32_t rot, pairs;                 // rotated elements; pairs: neighbours are a pair, else e and e + rot / 2
     int32_t q_aligned;                  // q may be read in 16-byte pieces
     int32_t wave_heads;                 // query heads of a token that a wave takes
+    int32_t words;                      // drafted trees: 64-bit words of a row of `sees`
+    const uint64_t *sees;               // which drafted tokens each of them sees: its depth, and so its position
 };
 #define PKV_MAX_ROTARY 64
+
+// What queries see of their contexts where that is not all up to their own token.
+#define PKV_TREE_WORDS 4                // 64-bit words of a row of a drafted tree's mask at most
+#define PKV_NO_WINDOW (1 << 28)         // (contexts end at 2^24 tokens)
+struct MaskArgs {
+    int32_t window, sinks;
+    int32_t words;                      // drafted trees
+    const uint64_t *sees;               // [query tokens][words]
+};
 
 // The ranges of a launch of kv_gather: rows and units (pages touched) of list entry i, its sequence and first token.
 struct GatherPlan {
@@ -267,3 +278,9 @@ hipError_t pkv_launch_prefill_prefixed(const AttnDesc &d, const ChunkPlan &plan,
 hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);
 // small calls of the same, by whole contexts; d as for a launch of the small decode kernel, at most PKV_PLAN_FEW sequences
 hipError_t pkv_launch_prefixed_small(const AttnDesc &d, const SharedRows &shared, hipStream_t s);
+// attention with windows and sinks: a decode step (d.parts, d.part_pages as for a small launch), chunks, and drafted trees
+hipError_t pkv_launch_window(const AttnDesc &d, const MaskArgs &mk, hipStream_t s);
+hipError_t pkv_launch_masked(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, hipStream_t s);
+// drafted tokens that stay: plan as of a chunk, without units; d addresses layer 0 of `layers`
+hipError_t pkv_launch_kv_keep(const AttnDesc &d, const ChunkPlan &plan, int layers, size_t layer_bytes, const int32_t *kept, const int32_t *n_kept,
+                              int32_t *new_lens, hipStream_t s);

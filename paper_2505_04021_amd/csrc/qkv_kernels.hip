@@ -487,7 +487,15 @@ __global__ __launch_bounds__(64) void k_qkv_append(const AttnDesc d, const QkvAr
 // back, 21.0, 19.6.)
 constexpr int QKV_WAVES = 4;
 
-template <int D, int DT, int SEQS>
+// How many drafted tokens, of its sequence's n, are in front of one on its path.
+__device__ __forceinline__ int depth_of(const uint64_t *row, int words, int n) {
+    const int seen = seen_drafts(row, words, n);
+    return seen > 0 ? seen - 1 : 0;
+}
+
+//
+// TREE: drafted tokens, whose positions go by how many drafted tokens each sees (its row of a.sees).
+template <int D, int DT, int SEQS, bool TREE>
 __global__ __launch_bounds__(64 * QKV_WAVES, 4) void k_qkv_append_chunk(const AttnDesc d, const QkvArgs a, const PlanOf<SEQS> plan) {
     constexpr int E = DT == PKV_BF16 ? 2 : 1;
     const int lane = threadIdx.x & 63;
@@ -502,6 +510,9 @@ __global__ __launch_bounds__(64 * QKV_WAVES, 4) void k_qkv_append_chunk(const At
         if (row >= (int)(lanes.pick(lanes.row, n_seqs) & PKV_PLAN_ROWS)) return;           // the last work-group may have waves to spare
         turn_queries(d, a, row, (x % per) * a.wave_heads, [&]() __attribute__((always_inline)) {
             const PlanUnit pu = lanes.find_row(plan, (uint32_t)row);
+            if constexpr (TREE)
+                return (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + PKV_CONST(int32_t, d.ctx_lens)[pu.seq] - pu.rows +
+                       depth_of(a.sees + (size_t)row * a.words, a.words, pu.rows);
             return (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + PKV_CONST(int32_t, d.ctx_lens)[pu.seq] - pu.rows + row - pu.row;
         });
         return;
@@ -553,7 +564,12 @@ __global__ __launch_bounds__(64 * QKV_WAVES, 4) void k_qkv_append_chunk(const At
         page_of(std::true_type{}, AsTheyAre{});
         return;
     }
-    const int pos = (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + page * PKV_T + (lane & 15);
+    int pos = (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + page * PKV_T + (lane & 15);
+    if constexpr (TREE) {
+        int i = page * PKV_T + (lane & 15) - tok0;         // (a slot that gets no token takes the position of one that does)
+        i = i < 0 ? 0 : (i < pu.rows ? i : pu.rows - 1);
+        pos = (a.before ? PKV_CONST(int32_t, a.before)[pu.seq] : 0) + tok0 + depth_of(a.sees + (size_t)(pu.row + i) * a.words, a.words, pu.rows);
+    }
     if (a.pairs) page_of(std::false_type{}, TurnKeys<D, true>(a, pos));
     else page_of(std::false_type{}, TurnKeys<D, false>(a, pos));
 }
@@ -568,16 +584,16 @@ hipError_t pkv_launch_qkv_append(const AttnDesc &d, const QkvArgs &a, hipStream_
     return hipGetLastError();
 }
 
-template <int SEQS>
+template <int SEQS, bool TREE>
 static void launch_chunk(const AttnDesc &d, const QkvArgs &a, const PlanOf<SEQS> &plan, dim3 grid, hipStream_t s) {
     static_assert(sizeof(AttnDesc) + sizeof(QkvArgs) + sizeof(PlanOf<SEQS>) <= 4096, "a kernel's arguments end at 4 KB");
     const dim3 wg(64 * QKV_WAVES);
     if (d.dtype == PKV_BF16) {
-        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_BF16, SEQS>), grid, wg, 0, s, d, a, plan);
-        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_BF16, SEQS>), grid, wg, 0, s, d, a, plan);
+        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_BF16, SEQS, TREE>), grid, wg, 0, s, d, a, plan);
+        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_BF16, SEQS, TREE>), grid, wg, 0, s, d, a, plan);
     } else {
-        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_E4M3, SEQS>), grid, wg, 0, s, d, a, plan);
-        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_E4M3, SEQS>), grid, wg, 0, s, d, a, plan);
+        if (d.D == 128) hipLaunchKernelGGL((k_qkv_append_chunk<128, PKV_E4M3, SEQS, TREE>), grid, wg, 0, s, d, a, plan);
+        else hipLaunchKernelGGL((k_qkv_append_chunk<64, PKV_E4M3, SEQS, TREE>), grid, wg, 0, s, d, a, plan);
     }
 }
 
@@ -587,7 +603,12 @@ hipError_t pkv_launch_qkv_append_chunk(const AttnDesc &d, const QkvArgs &a, cons
     if (rows == 0) return hipSuccess;
     if (waves > 0x7fffffffu) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)((waves + QKV_WAVES - 1) / QKV_WAVES));
-    if (plan.n_seqs <= PKV_PLAN_FEW) launch_chunk(d, a, few_of(plan), grid, s);
-    else launch_chunk(d, a, plan, grid, s);
+    if (plan.n_seqs <= PKV_PLAN_FEW) {
+        if (a.sees) launch_chunk<PKV_PLAN_FEW, true>(d, a, few_of(plan), grid, s);
+        else launch_chunk<PKV_PLAN_FEW, false>(d, a, few_of(plan), grid, s);
+    } else {
+        if (a.sees) launch_chunk<PKV_PLAN_SEQS, true>(d, a, plan, grid, s);
+        else launch_chunk<PKV_PLAN_SEQS, false>(d, a, plan, grid, s);
+    }
     return hipGetLastError();
 }
