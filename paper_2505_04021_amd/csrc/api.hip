@@ -351,6 +351,7 @@ constexpr int kDefaultSegCost = 6;
 constexpr double kPageCost = 0.8, kDeepPageCost = 1.6;
 int g_plan_items = kDefaultItems;     // items of the launch being prepared, all models together
 AttnForm g_last_form = AttnForm::ordinary;  // what the most recent launch ran as
+int g_mask_form = -1, g_last_mask_form = 0;       // chunks and trees under masks: 0 units of 16 columns, 1 groups of 128, -1 by the call
 int g_prefix_form = -1, g_last_prefix_form = 0;   // decode_attention_prefix: 0 prefixes once for all, 1 contexts whole, -1 by the call
 int g_last_prefill_parts = 0;         // most parts a context came in, in the most recent prefill_attention call
 int g_last_items = 0;                 // its work items, work-groups of a small launch
@@ -841,6 +842,14 @@ int pkv_set_prefix_form(int form) {
 }
 
 int pkv_last_prefix_form(void) { return g_last_prefix_form; }
+
+int pkv_set_mask_form(int form) {
+    if (form < -1 || form > 1) return PKV_E_ARG;
+    g_mask_form = form;
+    return PKV_OK;
+}
+
+int pkv_last_mask_form(void) { return g_last_mask_form; }
 
 int pkv_set_segment_cost(int pages) {
     if (pages < -1 || pages > 256) return PKV_E_ARG;
@@ -2560,26 +2569,56 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
     MaskArgs mk = mask_args(window, sinks);
     mk.sees = sees;
     mk.words = words;
-    const int group = 16 / m->g;
-    int64_t groups = 0;
-    int longest = 1;
-    for (int s = 0; s < batch; ++s) {
-        groups += (q_lens[s] + group - 1) / group;
-        const int pages = q_lens[s] ? masked_pages(m->row_len[s], mk.window, mk.sinks, group) : 0;
-        longest = longest > pages ? longest : pages;
+    // Few columns a kv head: units of 16, whose four waves walk different pages; else groups of 128, whose waves walk the same pages with 32 each.
+    int most = 0;
+    for (int s = 0; s < batch; ++s) most = most > q_lens[s] ? most : q_lens[s];
+    const bool narrow = g_mask_form >= 0 ? g_mask_form == 0 && total <= 1 << 16 : most * m->g <= 16;
+    g_last_mask_form = narrow ? 0 : 1;
+    const int tile = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g, group = narrow ? 16 / m->g : PKV_PREFILL_WAVES * tile;
+    auto pages_of = [&](int s) { return masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < group ? q_lens[s] : group); };
+    PlanBuilder plan(batch, PKV_PLAN_FEW);
+    if (narrow) {
+        int64_t groups = 0;
+        int longest = 1;
+        for (int s = 0; s < batch; ++s) {
+            groups += (q_lens[s] + group - 1) / group;
+            if (q_lens[s] > 0 && pages_of(s) > longest) longest = pages_of(s);
+        }
+        const int64_t slots = (int64_t)(m->ws_floats / partial_floats(16, m->D));
+        d.part_pages = masked_part_pages(groups * m->Hkv, longest, slots < (int64_t)m->cnt_cap ? slots : (int64_t)m->cnt_cap);
+        for (int s = 0; s < batch; ++s) {
+            if (plan.full()) HIP_TRY(pkv_launch_masked(d, mk, plan.take(s), tree, g_stream));
+            const int pages = pages_of(s), n = (q_lens[s] + group - 1) / group;
+            const int parts = pages > d.part_pages ? (pages + d.part_pages - 1) / d.part_pages : 1;
+            plan.add((uint32_t)q_lens[s], (uint32_t)(n * parts), (uint32_t)parts, (uint32_t)(pages / parts));
+        }
+        HIP_TRY(pkv_launch_masked(d, mk, plan.take(batch), tree, g_stream));
+        return PKV_OK;
     }
-    if (groups * kSmallMaxParts >= 1 << 22) return PKV_E_RANGE;
-    const int64_t slots = (int64_t)(m->ws_floats / partial_floats(16, m->D));
-    d.part_pages = masked_part_pages(groups * m->Hkv, longest, slots < (int64_t)m->cnt_cap ? slots : (int64_t)m->cnt_cap);
-    PlanBuilder plan(batch);
+    d.cols = tile * m->g;
+    int split_groups = 0;
+    auto launch = [&](const ChunkPlan &p) -> int {
+        if (split_groups > 0) {
+            const int rc = ensure_prefix_ws(*m, (size_t)p.s[p.n_seqs].unit * m->Hkv * PKV_PREFILL_COLS * (size_t)(m->D + 4), &d.ws);
+            if (rc) return rc;
+        }
+        HIP_TRY(pkv_launch_masked_wide(d, mk, p, tree, split_groups, g_stream));
+        split_groups = 0;
+        return PKV_OK;
+    };
+    double part_pairs = 0.0;
     for (int s = 0; s < batch; ++s) {
-        if (plan.full()) HIP_TRY(pkv_launch_masked(d, mk, plan.take(s), tree, g_stream));
-        const int pages = masked_pages(m->row_len[s], mk.window, mk.sinks, group), n = (q_lens[s] + group - 1) / group;
-        const int parts = pages > d.part_pages ? (pages + d.part_pages - 1) / d.part_pages : 1;
-        plan.add((uint32_t)q_lens[s], (uint32_t)(n * parts), (uint32_t)parts, (uint32_t)(pages / parts));
+        if (plan.full()) {
+            const int rc = launch(plan.take(s));
+            if (rc) return rc;
+        }
+        if (s % plan.per_launch == 0)
+            part_pairs = prefill_part_pairs(*m, s, s + plan.per_launch < batch ? s + plan.per_launch : batch, q_lens, group, pages_of);
+        const int parts = prefill_parts(pages_of(s), part_pairs), groups = (q_lens[s] + group - 1) / group;
+        plan.add((uint32_t)q_lens[s], (uint32_t)(groups * parts), (uint32_t)parts, (uint32_t)(pages_of(s) / parts));
+        if (parts > 1 && groups > split_groups) split_groups = groups;
     }
-    HIP_TRY(pkv_launch_masked(d, mk, plan.take(batch), tree, g_stream));
-    return PKV_OK;
+    return launch(plan.take(batch));
 }
 
 int prefill_attention_window(int model, int batch, const void *q, const int32_t *q_lens, const int32_t *ctx_lens, int window, int sinks, float *out) {

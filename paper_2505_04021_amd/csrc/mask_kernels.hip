@@ -1,6 +1,7 @@
 // Attention with sliding windows and sinks, and of drafted trees, over the paged cache (gfx950).  mask_part.h says what is seen and how a
 // context is walked.
 #include "mask_part.h"
+#include "prefill_groups.h"
 
 namespace {
 
@@ -62,6 +63,95 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d
     masked_part<D, DT, TREE>(d, mk, u, s_acc, s_m, s_l, s_mask, &s_arrived);
 }
 
+// Groups of up to 128 columns (prefill_unit.h): a group of query tokens, four waves with 32 columns each, or one of the parts of what it sees.
+template <bool TREE>
+struct MaskedGroup {
+    static constexpr bool CAUSAL = false, LEVELS = true, SHARED = false, MASKED = true;
+    const MaskArgs &mk;
+    int seq, q0, ntok, part, parts, slot;
+    const int32_t *own;
+    uint32_t *rows;                                       // LDS: rows of a tree's mask, by wave and token of its tile
+    int drafts, pos0, base;                               // tokens of the sequence's chunk; position of the group's first; TREE: drafts begin there, along the walk
+    Walk walk;
+
+    __device__ __forceinline__ MaskedGroup(const GroupInfo &g, const AttnDesc &d, const MaskArgs &mk, int group, int chunk, uint32_t *rows)
+        : mk(mk), seq(g.seq), q0(g.q0), ntok(g.ntok), part(g.part), parts(g.parts), slot(group), own(d.table + (size_t)g.seq * d.row_stride), rows(rows), drafts(chunk) {
+        int ctx = PKV_CONST(int32_t, d.ctx_lens)[seq], cap = PKV_CONST(int32_t, d.row_len)[seq];
+        asm volatile("" : "+s"(ctx), "+s"(cap));          // both at once
+        cap *= PKV_T;
+        if constexpr (TREE) {
+            base = pos0 = ctx - chunk;
+            const int L = base < 0 ? 0 : (ctx < cap ? ctx : cap);
+            walk = walk_of(L, base + 1 - mk.window, base + chunk - mk.window, base, mk.sinks);
+            base -= walk.skip * PKV_T;
+        } else {
+            const int L = ctx < 0 ? 0 : (ctx < cap ? ctx : cap);
+            pos0 = L - g.back - ntok;
+            base = 0;
+            walk = walk_of(pos0 + ntok, pos0 + 1 - mk.window, pos0 + ntok - mk.window, pos0 + 1, mk.sinks);
+        }
+    }
+    __device__ __forceinline__ int front() const { return 0; }
+    __device__ __forceinline__ uint32_t id(const AttnDesc &d, int page) const {
+        const int at = walk.page(page);
+        return (uint32_t)own[at < d.row_stride ? at : d.row_stride - 1];
+    }
+    __device__ __forceinline__ int row(int i) const { return q0 + i; }
+    __device__ __forceinline__ int sees(const AttnDesc &) const { return walk.len; }
+    __device__ __forceinline__ bool partial() const { return parts > 1; }
+    __device__ __forceinline__ size_t tile(const AttnDesc &d, int kvh, int w) const { return ((size_t)slot * d.Hkv + kvh) * PF_WAVES + w; }
+    // tokens at the walk's end that none of the group's queries sees but the last k
+    __device__ __forceinline__ int behind(int k) const { return TREE ? 0 : k; }
+    // what query i sees, token t of wave w's tile: sinks, tokens from `from` on below `upto`, and those of the row that is returned
+    __device__ __forceinline__ uint32_t *column(int w, int t, int i, int &from, int &upto) const {
+        if constexpr (TREE) {
+            uint32_t *row = rows + (w * PF_COLS + t) * MASK_WORDS;
+            const uint64_t *bits = mk.sees + (size_t)(q0 + i) * mk.words;
+            const int n = seen_drafts(bits, mk.words, drafts);
+            for (int k = 0; k < mk.words; ++k) {
+                const uint64_t x = bits[k];
+                row[2 * k] = (uint32_t)x;
+                row[2 * k + 1] = (uint32_t)(x >> 32);
+            }
+            upto = base;
+            from = base + (n > 0 ? n : 1) - mk.window;
+            return row;
+        }
+        upto = pos0 + i + 1 - walk.skip * PKV_T;
+        from = upto - mk.window;
+        return nullptr;
+    }
+    __device__ __forceinline__ uint32_t seen(int x0, int from, int upto, const uint32_t *row) const {
+        uint32_t bits = seen_bits(x0, upto, from, walk.sinks);
+        if constexpr (TREE) bits |= row_bits(row, 2 * mk.words, x0 - base);
+        return bits & below(walk.len - x0);
+    }
+};
+
+template <int D, int DT, int MEET, bool TREE, int SEQS>
+__global__ __launch_bounds__(64 * PF_WAVES, 2) void k_masked_wide(const AttnDesc d, const MaskArgs mk, const PlanOf<SEQS> plan) {
+    __shared__ __align__(16) uint8_t ring[kRingBytes<D, DT, MEET>];
+    __shared__ uint32_t rows[TREE ? PF_WAVES * PF_COLS * MASK_WORDS : 1];
+    const PlanLanes<SEQS> lanes(plan);
+    ask_arguments(d, plan.n_seqs, plan.seq0);
+    const int group = blockIdx.x / d.Hkv, kvh = blockIdx.x - group * d.Hkv;
+    const GroupInfo gi = group_info(d, plan, lanes, group);
+    prefill_unit<D, DT, MEET, true>(d, MaskedGroup<TREE>(gi, d, mk, group, lanes.find(plan, (uint32_t)group).rows, rows), kvh, ring);
+}
+
+template <bool TREE, int SEQS>
+void launch_wide(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan, int split_groups, hipStream_t s) {
+    const dim3 grid(plan.s[plan.n_seqs].unit * (unsigned)d.Hkv), wg(64 * PF_WAVES);
+    if (d.dtype == PKV_BF16) {
+        if (d.D == 128) hipLaunchKernelGGL((k_masked_wide<128, PKV_BF16, 2, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        else hipLaunchKernelGGL((k_masked_wide<64, PKV_BF16, 2, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+    } else {
+        if (d.D == 128) hipLaunchKernelGGL((k_masked_wide<128, PKV_E4M3, 4, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        else hipLaunchKernelGGL((k_masked_wide<64, PKV_E4M3, 4, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+    }
+    if (split_groups > 0) launch_merge(d, plan, split_groups, s);
+}
+
 template <bool TREE, int SEQS>
 void launch(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan, hipStream_t s) {
     static_assert(sizeof(AttnDesc) + sizeof(MaskArgs) + sizeof(plan) <= 4096, "a kernel's arguments end at 4 KB");
@@ -91,12 +181,16 @@ hipError_t pkv_launch_window(const AttnDesc &d, const MaskArgs &mk, hipStream_t 
 
 hipError_t pkv_launch_masked(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, hipStream_t s) {
     if (plan.s[plan.n_seqs].unit == 0) return hipSuccess;
-    if (plan.n_seqs <= PKV_PLAN_FEW) {
-        if (tree) launch<true>(d, mk, few_of(plan), s);
-        else launch<false>(d, mk, few_of(plan), s);
-    } else {
-        if (tree) launch<true>(d, mk, plan, s);
-        else launch<false>(d, mk, plan, s);
-    }
+    const auto few = few_of(plan);
+    if (tree) launch<true>(d, mk, few, s);
+    else launch<false>(d, mk, few, s);
+    return hipGetLastError();
+}
+
+hipError_t pkv_launch_masked_wide(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, int split_groups, hipStream_t s) {
+    if (plan.s[plan.n_seqs].unit == 0) return hipSuccess;
+    const auto few = few_of(plan);
+    if (tree) launch_wide<true>(d, mk, few, split_groups, s);
+    else launch_wide<false>(d, mk, few, split_groups, s);
     return hipGetLastError();
 }

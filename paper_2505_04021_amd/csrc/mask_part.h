@@ -1,64 +1,9 @@
-// Which tokens a query sees where that is not simply "all up to its own" (gfx950): a sliding window with sinks, or the ancestors of a
-// drafted token behind its context; and the work-group that walks one part of such a context for up to 16 columns.
-//
-//   out = softmax over the seen t of (q . k_t / sqrt D) V
-//
-// A query at position p sees token t <= p where t > p - window or t < sinks.  A drafted token sees the cached tokens in front of the drafts by the
-// same rule, p being the position that its depth gives it, and of the drafted ones those whose bit is set in its row of the mask.
+// Attention under masks (mask_walk.h): the work-group that walks one part of a context for up to 16 columns (gfx950).
 #pragma once
 #include "decode_part.h"
+#include "mask_walk.h"
 
 namespace {
-
-// The tokens that some query of a unit may see, as one walk along pages: the sinks' pages, then those from the first query's window on.
-// Tokens are counted along the walk: those behind the gap are 16 * skip fewer than in the row.
-struct Walk {
-    int len;                 // tokens, to the end of what the last query sees
-    int front, skip;         // pages in front of the gap; pages left out
-    int sinks;               // tokens in front that every query sees
-    int lo_min, lo_max;      // where the windows of the first and of the last query begin
-    int hi_min;              // tokens that all queries see, but for the windows
-    __device__ __forceinline__ int page(int i) const { return i < front ? i : i + skip; }
-    __device__ __forceinline__ int pages() const { return (len + PKV_T - 1) / PKV_T; }
-    // whether every query sees all 32 tokens of pair p
-    __device__ __forceinline__ bool plain(int x0) const { return (x0 + 32 <= hi_min) & ((x0 >= lo_max) | (x0 + 32 <= sinks)); }
-};
-
-// L tokens of the row; windows that begin at token `lo_min` and `lo_max`; all queries see tokens below `hi_min`, as far as windows go
-__device__ __forceinline__ Walk walk_of(int L, int lo_min, int lo_max, int hi_min, int sinks) {
-    Walk w;
-    L = L < 0 ? 0 : L;
-    auto within = [&](int x) __attribute__((always_inline)) { return x < 0 ? 0 : (x < L ? x : L); };
-    w.sinks = within(sinks);
-    lo_min = within(lo_min);
-    w.front = (w.sinks + PKV_T - 1) / PKV_T;
-    const int first = lo_min / PKV_T;
-    w.skip = first > w.front ? first - w.front : 0;
-    const int shift = w.skip * PKV_T;
-    w.len = L - shift;
-    w.lo_min = lo_min - shift;
-    w.lo_max = within(lo_max) - shift;
-    w.hi_min = within(hi_min) - shift;
-    return w;
-}
-
-// bits 0 .. n - 1
-__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); }
-
-// A column's 32 tokens from x0 on: seen are those below `hi` that are sinks or not below `lo`
-__device__ __forceinline__ uint32_t seen_bits(int x0, int hi, int lo, int sinks) {
-    return below(hi - x0) & (~below(lo - x0) | below(sinks - x0));
-}
-
-// Rows of a tree's mask in LDS: bits [from, from + 32) of a row of `words` 32-bit words, zeros beyond it
-__device__ __forceinline__ uint32_t row_bits(const uint32_t *row, int words, int from) {
-    const int i = from >> 5;                              // (arithmetic: -1 for the 32 bits in front)
-    auto word = [&](int k) __attribute__((always_inline)) {
-        const uint32_t x = row[k < 0 ? 0 : (k < words ? k : words - 1)];
-        return k >= 0 && k < words ? x : 0u;
-    };
-    return __builtin_amdgcn_alignbit(word(i + 1), word(i), (uint32_t)from & 31u);
-}
 
 // One work-group's part of a launch: up to 16 columns, `tokens` query tokens x the g heads of a kv head.
 struct MaskUnit {
@@ -73,13 +18,12 @@ struct MaskUnit {
 // Blanks the tokens of a V tile that no query sees, which may hold anything (even NaN); a set bit: seen
 template <int D, int DT>
 __device__ __forceinline__ void keep_v(u32x4 *v, uint32_t four) {
-    const uint32_t m01 = (four & 1u ? 0xffffu : 0u) | (four & 2u ? 0xffff0000u : 0u), m23 = (four & 4u ? 0xffffu : 0u) | (four & 8u ? 0xffff0000u : 0u);
-    const uint32_t m = (four & 1u ? 0xffu : 0u) | (four & 2u ? 0xff00u : 0u) | (four & 4u ? 0xff0000u : 0u) | (four & 8u ? 0xff000000u : 0u);       // codes
+    const uint32_t m01 = halves_of(four), m23 = halves_of(four >> 2), m = bytes_of(four);
 #pragma unroll
     for (int j = 0; j < Tile<D, DT>::NL; ++j) v[j] &= DT == PKV_BF16 ? mk4(m01, m23, m01, m23) : mk4(m, m, m, m);
 }
 
-constexpr int MASK_COLS = 16, MASK_WORDS = 2 * PKV_TREE_WORDS;      // columns of a unit; 32-bit words of a row of a tree's mask
+constexpr int MASK_COLS = 16;                             // columns of a unit
 
 // The work-group's four waves take the page pairs of its part in turn and join their sums through LDS; the last of several parts to arrive joins
 // those through memory (as attn_part in decode_part.h, whose comments say why it is built like this).
@@ -229,7 +173,7 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
                 if (!(mine >> i & 1u)) s[i] = -INFINITY;
                 if (!(mine >> (16 + i) & 1u)) s[4 + i] = -INFINITY;
             }
-            const uint32_t any = (there & seen_bits(x0, walk.len, walk.lo_min, walk.sinks)) >> (4 * G);
+            const uint32_t any = (there & walk.some(x0)) >> (4 * G);
             keep_v<D, DT>(r.a.v, any);
             keep_v<D, DT>(r.b.v, any >> 16);
         }

@@ -2,7 +2,7 @@
 // head), over the page pairs of a unit.  Which tokens, which blocks and where the sums go is said by the unit (k_prefill and
 // its like, whose file comments say what bounds it and why it has this shape).
 #pragma once
-#include "mfma_util.h"
+#include "mask_walk.h"
 
 namespace {
 
@@ -72,6 +72,8 @@ constexpr int kRingBytes = 2 * (2 * MEET) * 2 * PfTile<D, DT>::BYTES;
 //   partial()                  whether sums go to d.ws for a later join, or rows to out
 //   SHARED, front()            whether contexts begin with tokens of another row, and how many: every query sees at least those
 //   CAUSAL                     token i sees ntok - 1 - i tokens fewer than the last one; otherwise all see the same
+//   MASKED                     which tokens are seen is said by the unit's walk, and for each query by column() and, of drafted trees, by the rows of a
+//                              mask that column() leaves in LDS
 // LOW: probabilities reach the matrix unit with 16 significant bits (bf16 high and low halves), else with 8.
 template <int D, int DT, int MEET, bool LOW, typename UNIT>
 __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, int kvh, uint8_t *ring) {
@@ -116,10 +118,27 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     const int least = UNIT::SHARED ? (u.front() < L ? u.front() : L) : 0;
     auto at_least = [&](int sees) __attribute__((always_inline)) { return UNIT::SHARED && sees < least ? least : sees; };
     const int causal_from = at_least(UNIT::CAUSAL ? L - (ntok - 1) : L);
-    const int p_plain = causal_from > 0 ? causal_from >> 5 : 0;
+    int p_plain = causal_from > 0 ? causal_from >> 5 : 0, p_first = 0;      // masks in front of pair p_first and from p_plain on
 
     const int col_lim = at_least(UNIT::CAUSAL && col_live ? L - (ntok - 1 - (t0 + tok)) : L);        // tokens this column sees
-    const int tile_lim = my_tok > 0 ? at_least(L - (UNIT::CAUSAL ? ntok - t0 - my_tok : 0)) : 0;     // tokens some column of the tile sees
+    int tile_lim = my_tok > 0 ? at_least(L - (UNIT::CAUSAL ? ntok - t0 - my_tok : 0)) : 0;     // tokens some column of the tile sees
+    // MASKED: this lane's column sees sinks and tokens from `from` on below `upto`, and those of its row of a mask
+    int from = 0, upto = 0;
+    uint32_t *mask_row = nullptr;
+    if constexpr (UNIT::MASKED) {
+        // (a column that stands for no query has the tile's first token's, or, in a tile without any, the unit's last one's)
+        const int t = col_live ? tok : 0, i = t0 + t;
+        mask_row = u.column(w, t, i < ntok ? i : ntok - 1, from, upto);
+        p_first = (u.walk.lo_max + 31) >> 5;
+        p_plain = u.walk.hi_min >> 5;
+        tile_lim = my_tok > 0 ? L - u.behind(ntok - t0 - my_tok) : 0;
+    }
+    auto seen = [&](int p) __attribute__((always_inline)) {           // of pair p, from this lane's first token on
+        if constexpr (UNIT::MASKED) return u.seen(32 * p, from, upto, mask_row) >> (4 * h);
+        else return 0u;
+    };
+    // whether a pair's token i (of this lane's sixteen) is one that its column does not see
+    auto unseen = [](uint32_t bits, int i) __attribute__((always_inline)) { return (bits >> (16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3)) & 1u) == 0u; };
 
     f32x16 acc[TL::ND];
 #pragma unroll
@@ -249,6 +268,28 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     };
     // tokens past the context may hold anything (even NaN): blank their V (their probabilities are 0)
     auto blank_v = [&](int p) __attribute__((always_inline)) {
+        if constexpr (UNIT::MASKED) {
+            const uint32_t some = u.walk.some(32 * p) >> (4 * h);      // those that some query of the unit sees
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t four = some >> (16 * k + 8 * q);
+                    if constexpr (DT == PKV_BF16) {
+                        const uint32_t m01 = halves_of(four), m23 = halves_of(four >> 2);
+#pragma unroll
+                        for (int dt = 0; dt < TL::ND; ++dt) {
+                            vr[dt][k][2 * q] &= m01;
+                            vr[dt][k][2 * q + 1] &= m23;
+                        }
+                    } else {
+                        const uint32_t mm = bytes_of(four);
+#pragma unroll
+                        for (int dt = 0; dt < TL::ND; ++dt) vr[dt][k][q] &= mm;
+                    }
+                }
+            return;
+        }
         const int left = L - 32 * p - 4 * h;               // tokens of the pair before the end, from this half's first
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -271,6 +312,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             }
     };
 
+    auto needs_mask = [&](int p) __attribute__((always_inline)) { return UNIT::MASKED ? (p < p_first) | (p >= p_plain) : p >= p_plain; };
     // ---- one pair's softmax, in two parts.  Arguments: t = score * scale - m (log2 domain) against the reference
     // point m as it stands.  m need not be the column's maximum, only near it: it moves, and the sums are
     // rescaled, when a lane's sum of the pair's probabilities exceeds kSumBar, so that no probability does.
@@ -291,7 +333,16 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
 #pragma unroll
             for (int i = 0; i < 16; ++i) pr[i] = __builtin_fmaf(s[i], i < 8 ? sca : scb, -m);
         }
-        if (masked) {
+        if constexpr (UNIT::MASKED) {
+            if (masked) {
+                const uint32_t bits = seen(p);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = pr[i];
+                    pr[i] = unseen(bits, i) ? -INFINITY : x;
+                }
+            }
+        } else if (masked) {
             const int rel = col_lim - 32 * p - 4 * h;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -313,11 +364,12 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
         if (__builtin_expect(__any(sum > bar), 0)) {
             // the column's maximum from the scores themselves (arguments are inexact when m is far off)
             const int rel = col_lim - 32 * p - 4 * h;
+            const uint32_t bits = UNIT::MASKED && masked ? seen(p) : 0u;
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float x = s[i] * (i < 8 ? sca : scb);
-                const bool dead = masked && 16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3) >= rel;
+                const bool dead = masked && (UNIT::MASKED ? unseen(bits, i) : 16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3) >= rel);
                 top = fmaxf(top, dead ? -INFINITY : x);
             }
             top = halves_max(top);
@@ -422,32 +474,30 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             scores();
             sva = sva_n; svb = svb_n;
             if (np > 1) read_k(1);
-            const bool masked = p_begin >= p_plain;
+            const bool masked = needs_mask(p_begin);
             args(p_begin, masked);
             settle(p_begin, masked);
         }
         int r = 0;
         // pairs in front of pairs without masks: straight-line steps
         const int plain = live ? (np < p_plain - p_begin ? np : p_plain - p_begin) - 1 : 0;
-        if (plain > 0) {
-            do {
-                read_v(r);
-                scales(p_begin + r + 1);
-                scores();
-                probabilities();
-                if (!(r & (MEET - 1))) meet(r);
-                if (r + 2 < np) read_k(r + 2);
-                sva = sva_n; svb = svb_n;
-                accumulate(ph);
-                if (LOW) {
-                    low_halves();
-                    accumulate(pl);
-                }
-                args(p_begin + r + 1, false);
-                settle(p_begin + r + 1, false);
-            } while (++r < plain);
-        }
-        for (; r < np; ++r) {
+        auto plain_step = [&]() __attribute__((always_inline)) {
+            read_v(r);
+            scales(p_begin + r + 1);
+            scores();
+            probabilities();
+            if (!(r & (MEET - 1))) meet(r);
+            if (r + 2 < np) read_k(r + 2);
+            sva = sva_n; svb = svb_n;
+            accumulate(ph);
+            if (LOW) {
+                low_halves();
+                accumulate(pl);
+            }
+            args(p_begin + r + 1, false);
+            settle(p_begin + r + 1, false);
+        };
+        auto step = [&]() __attribute__((always_inline)) {
             const int p = p_begin + r;
             const bool now = 32 * p < tile_lim, next = (r + 1 < np) & (32 * (p + 1) < tile_lim);     // (neither where no token is the wave's)
             if (now) {
@@ -461,7 +511,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             if (r + 1 < np && !(r & (MEET - 1))) meet(r);
             if (next && r + 2 < np) read_k(r + 2);
             if (now) {
-                if (32 * (p + 1) > L) blank_v(p);
+                if (UNIT::MASKED ? needs_mask(p) : 32 * (p + 1) > L) blank_v(p);
                 accumulate(ph);
                 if (LOW) {
                     low_halves();
@@ -470,11 +520,19 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             }
             if (next) {
                 sva = sva_n; svb = svb_n;
-                const bool masked = p + 1 >= p_plain;
+                const bool masked = needs_mask(p + 1);
                 args(p + 1, masked);
                 settle(p + 1, masked);
             }
+        };
+        // masks at both ends of the walk (one loop around both kinds of step: the sums change registers between them, and 128-wide heads spill)
+        if constexpr (UNIT::MASKED)
+            for (; r < np && p_begin + r < p_first; ++r) step();
+        if (r < plain) {
+            do plain_step();
+            while (++r < plain);
         }
+        for (; r < np; ++r) step();
     }
 
     l += __shfl_xor(l, 32);
@@ -489,7 +547,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     };
     if (u.partial()) {
         // a part of the context: the unnormalised sums, the reference point and the denominator of every column
-        if (UNIT::CAUSAL || col_live) {
+        if (UNIT::CAUSAL || UNIT::MASKED || col_live) {
             float *part = d.ws + (u.tile(d, kvh, w) * PF_COLS + n) * (D + 4);
             put_sums(part, 1.f);
             if (h == 0) {

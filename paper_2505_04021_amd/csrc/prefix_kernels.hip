@@ -44,7 +44,7 @@ struct GroupShape {
 };
 
 struct PrefixUnit {
-    static constexpr bool CAUSAL = false, SHARED = false;
+    static constexpr bool CAUSAL = false, SHARED = false, MASKED = false;
     __device__ __forceinline__ int front() const { return 0; }
     // (96 rows behind 24576 tokens, without their own, in 192 work-groups 138, 146 us without levels, in 400 112.5, 115.7)
     static constexpr bool LEVELS = true;

@@ -8,6 +8,7 @@ import masked_ops as M
 import plain_ops as P
 from test_gpu_prefix import BF16, E4M3, SHAPES, Rows, gpu  # noqa: F401  (gpu: fixture)
 from test_gpu_qkv_append import close, inputs, weights
+from test_gpu_windows import form  # noqa: F401  (fixture)
 from workloads import gen
 
 pytestmark = pytest.mark.gpu
@@ -22,7 +23,7 @@ def attend(gpu, rows, q, masks, ctx, window=0, sinks=0, words=None):  # noqa: F8
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
-def test_trees(gpu, hq, hkv, d, dtype):  # noqa: F811
+def test_trees(gpu, form, hq, hkv, d, dtype):  # noqa: F811
     """Trees of no token, of one, of odd numbers and across the ends of pages and mask words, behind no context, short and long ones."""
     n = [1, 0, 5, 26, 60, 7, 64, 2, 33, 16]
     base = [0, 50, 0, 300, 1000, 31, 17, 16, 0, 700]
@@ -37,7 +38,7 @@ def test_trees(gpu, hq, hkv, d, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(16, 4, 128, BF16), (3, 3, 64, E4M3)])
-def test_any_mask(gpu, hq, hkv, d, dtype):  # noqa: F811
+def test_any_mask(gpu, form, hq, hkv, d, dtype):  # noqa: F811
     """Masks that are no trees: any bits, none, all; bits behind the drafts, which are not looked at; up to 256 drafted tokens; a context length below
     the number of drafts, and one beyond the row's blocks."""
     rng = np.random.default_rng(d)
@@ -55,7 +56,7 @@ def test_any_mask(gpu, hq, hkv, d, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(32, 8, 128, BF16), (8, 1, 64, BF16), (64, 8, 128, BF16), (16, 2, 128, E4M3), (4, 1, 64, E4M3)])
-def test_trees_behind_long_contexts(gpu, hq, hkv, d, dtype):  # noqa: F811
+def test_trees_behind_long_contexts(gpu, form, hq, hkv, d, dtype):  # noqa: F811
     """Few drafted tokens and many in front of contexts that are cut into parts."""
     n, base = [3, 40, 1], [9000, 5000, 12000]
     rng = np.random.default_rng(9)
@@ -70,7 +71,7 @@ def test_trees_behind_long_contexts(gpu, hq, hkv, d, dtype):  # noqa: F811
     rows.c.close()
 
 
-def test_chain_is_a_chunk(gpu):  # noqa: F811
+def test_chain_is_a_chunk(gpu, form):  # noqa: F811
     """A tree without branches sees what a chunk's queries see."""
     hq, hkv, d, n, base = 32, 8, 128, [7, 30, 1], [100, 0, 515]
     ctx = [a + b for a, b in zip(base, n)]
@@ -245,7 +246,7 @@ def test_refusals(gpu):  # noqa: F811
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (40, 4)])
-def test_drafted_and_verified(gpu, dtype, window, sinks):  # noqa: F811
+def test_drafted_and_verified(gpu, form, dtype, window, sinks):  # noqa: F811
     """Steps of speculative decoding as a layer goes through them: drafts appended, attended to, the accepted path kept, on and on.  In a bf16 cache the
     accepted tokens end up bit for bit as if they had been appended one by one, and their outputs are those of a decode step."""
     hq, hkv, d, batch, room = 8, 2, 128, 5, 200

@@ -13,6 +13,14 @@ pytestmark = pytest.mark.gpu
 WINDOWS = [(1, 0), (1, 1), (16, 0), (17, 4), (5, 40), (100, 4), (64, 16), (130, 33), (1000, 0), (1 << 30, 3), (2147483647, 2147483647)]
 
 
+@pytest.fixture(params=[0, 1], ids=["units of 16", "groups of 128"])
+def form(gpu, request):  # noqa: F811
+    """Both ways in which chunks and trees fall into work-groups."""
+    assert gpu.set_mask_form(request.param) == 0
+    yield request.param
+    gpu.set_mask_form(-1)
+
+
 def decode(gpu, rows, q, ctx, window, sinks):  # noqa: F811
     c = rows.c
     out = torch.full((len(ctx), c.hq, c.d), float("nan"), device="cuda")
@@ -54,7 +62,7 @@ def test_decode_wide_windows_of_few_rows(gpu, hq, hkv, d, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
-def test_prefill(gpu, hq, hkv, d, dtype):  # noqa: F811
+def test_prefill(gpu, form, hq, hkv, d, dtype):  # noqa: F811
     """Ragged chunks: none, one, around tiles, several windows long, behind nothing and behind long contexts; queries before their row."""
     n = [1, 0, 7, 33, 64, 150, 5, 300, 40, 16]
     ctx = [1, 20, 7, 50, 1000, 150, 999, 301, 25, 16]                    # row 8: 15 queries stand before position 0
@@ -71,7 +79,7 @@ def test_prefill(gpu, hq, hkv, d, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(32, 8, 128, BF16), (8, 1, 64, BF16), (16, 2, 128, E4M3)])
-def test_prefill_long(gpu, hq, hkv, d, dtype):  # noqa: F811
+def test_prefill_long(gpu, form, hq, hkv, d, dtype):  # noqa: F811
     """Prompts of many groups, and few queries whose wide window is cut into parts."""
     rows = Rows(gpu, hq, hkv, d, dtype, [1200, 9000, 700], frames=200)
     q = gen.queries((37, d), 1200 + 3 + 650, hq, d)
@@ -83,7 +91,7 @@ def test_prefill_long(gpu, hq, hkv, d, dtype):  # noqa: F811
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
 @pytest.mark.parametrize("d", [64, 128])
-def test_what_is_not_seen_may_hold_anything(gpu, d, value):  # noqa: F811
+def test_what_is_not_seen_may_hold_anything(gpu, form, d, value):  # noqa: F811
     """NaN and infinities in tokens between the sinks and the window, and (the pool is all NaN) behind the context."""
     hq, hkv, lens, window, sinks = 8, 2, [300, 77, 1000], 50, 5
     rows = Rows(gpu, hq, hkv, d, BF16, lens)
@@ -100,7 +108,7 @@ def test_what_is_not_seen_may_hold_anything(gpu, d, value):  # noqa: F811
     rows.c.close()
 
 
-def test_as_the_calls_without_windows(gpu):  # noqa: F811
+def test_as_the_calls_without_windows(gpu, form):  # noqa: F811
     """A window that covers everything: the rows of decode_attention and prefill_attention, up to the order of sums."""
     hq, hkv, d, lens = 32, 8, 128, [0, 5, 600, 2000, 31]
     rows = Rows(gpu, hq, hkv, d, BF16, lens, frames=60)
@@ -116,7 +124,7 @@ def test_as_the_calls_without_windows(gpu):  # noqa: F811
     rows.c.close()
 
 
-def test_many_sequences(gpu):  # noqa: F811
+def test_many_sequences(gpu, form):  # noqa: F811
     """More sequences than a launch's plan holds."""
     hq, hkv, d, n = 4, 1, 64, 1000
     rng = np.random.default_rng(6)
