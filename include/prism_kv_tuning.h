@@ -56,10 +56,10 @@ int pkv_last_launch_items(void);
 int pkv_set_prefix_form(int form);
 /* Which of the two the most recent call took (0 or 1). */
 int pkv_last_prefix_form(void);
-/* How prefill_attention_window and tree_attention fall into work-groups: 0 by units of 16 columns (query tokens x heads of a kv head; not beyond 65536
- * query tokens), 1 by groups of 128, -1 (the start) by what the call brings. */
+/* How prefill_attention_window and tree_attention fall into work-groups: 0 by units of 16 columns (query tokens x heads of a kv head), 1 by groups
+ * of 128, 2 by units of 32 (1 beyond 65536 query tokens), -1 (the start) by what the call brings. */
 int pkv_set_mask_form(int form);
-/* Which of the two the most recent call took (0 or 1). */
+/* Which of the three the most recent call took. */
 int pkv_last_mask_form(void);
 /* The most parts a sequence's context came in, in the most recent prefill_attention call (1: none was cut). */
 int pkv_last_prefill_parts(void);

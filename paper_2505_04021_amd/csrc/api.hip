@@ -324,6 +324,7 @@ void free_model_dev(Model &m) {
 // ordinary form (123 against 155 us for 620 MB).  Launches of fewer than 10 240 page units are left to
 // the ordinary form as well (within a microsecond either way, mostly in its favour).
 constexpr int kDefaultItems = 2048;
+constexpr int kMaskPartials = 1024;           // work-groups of 32 columns whose partial sums the split-K workspace holds
 constexpr int kDeepMaxItems = 1024, kDeepMinItems = 512, kItemGrain = 256;
 constexpr double kDeepMinUnits = 10240.0;
 constexpr double kMemBytesPerUs = 6.6e6;       // what the memory system delivers to this kernel at its best
@@ -336,6 +337,7 @@ constexpr double kDeepCapacity = 1.3;          // waves' own rate over the memor
 // 40 x 460 (13 400) 27.3 -> 29.3, 16 x 2048 (24 300) 40.4 -> 42.6; e4m3 8 x 2048 19.8 -> 11.8 and, 64-wide, 19.9 -> 9.6.
 // The line lies where the two meet in bf16; e4m3 launches of some more pages (20 x 1000, 11 800: 20.1, 15.5) would still be faster here.
 constexpr double kSmallMaxPages = 11000.0;
+constexpr int kMaskPart[] = {24, 32, 40, 56, 72, 96, 128, 176, 240, 320, 440, 640, 1024};
 constexpr int kSmallPart[] = {24, 32, 40, 64, 96, 128, 256, PKV_MAX_ROW_BLOCKS}, kSmallMaxParts = 64;
 constexpr long kSmallWorkGroups = 512, kSmallCUs = 256;         // work-groups that the chip holds at once, one to a CU
 // Smallest share of a wave, in pages.  It only binds in launches too small to give every wave slot a
@@ -351,7 +353,7 @@ constexpr int kDefaultSegCost = 6;
 constexpr double kPageCost = 0.8, kDeepPageCost = 1.6;
 int g_plan_items = kDefaultItems;     // items of the launch being prepared, all models together
 AttnForm g_last_form = AttnForm::ordinary;  // what the most recent launch ran as
-int g_mask_form = -1, g_last_mask_form = 0;       // chunks and trees under masks: 0 units of 16 columns, 1 groups of 128, -1 by the call
+int g_mask_form = -1, g_last_mask_form = 0;       // chunks and trees under masks: 0 units of 16 columns, 1 groups of 128, 2 units of 32, -1 by the call
 int g_prefix_form = -1, g_last_prefix_form = 0;   // decode_attention_prefix: 0 prefixes once for all, 1 contexts whole, -1 by the call
 int g_last_prefill_parts = 0;         // most parts a context came in, in the most recent prefill_attention call
 int g_last_items = 0;                 // its work items, work-groups of a small launch
@@ -844,7 +846,7 @@ int pkv_set_prefix_form(int form) {
 int pkv_last_prefix_form(void) { return g_last_prefix_form; }
 
 int pkv_set_mask_form(int form) {
-    if (form < -1 || form > 1) return PKV_E_ARG;
+    if (form < -1 || form > 2) return PKV_E_ARG;
     g_mask_form = form;
     return PKV_OK;
 }
@@ -1310,7 +1312,8 @@ int model_register_layers(int pool, int q_heads, int kv_heads, int head_dim, int
     // this model, so that decode_attention* neither waits nor allocates (graph capture needs no
     // priming launch)
     {
-        const int rc = ensure_workspace(m, ws_floats_for(m, kDefaultItems, m.g), (size_t)max_seqs * kv_heads, 1);
+        const size_t decode = ws_floats_for(m, kDefaultItems, m.g), masked = (size_t)kMaskPartials * partial_floats(32, m.D);
+        const int rc = ensure_workspace(m, decode > masked ? decode : masked, (size_t)max_seqs * kv_heads, 1);
         if (rc) {
             free_model_dev(m);
             return rc;
@@ -2486,6 +2489,7 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
 
 /* ------------------------------------------------ windows and drafted trees */
 
+
 // Pages that the last query of a sequence walks, as far as the host knows.
 static int masked_pages(int pages, int window, int sinks, int queries) {
     const int64_t most = (int64_t)(sinks + 15) / 16 + ((int64_t)window + queries + 15) / 16 + 1;
@@ -2504,16 +2508,85 @@ static void masked_desc(AttnDesc &d, const Model &m, int batch, const void *q, c
     d.cnt = m.cnt;
 }
 
-// Pages of a part where `units` work-groups would walk up to `longest` pages uncut.
-static int masked_part_pages(int64_t units, int longest, int64_t most_units) {
-    int64_t parts = units > 0 ? kSmallWorkGroups / units : 1;
-    if (parts > longest / kSmallPart[0]) parts = longest / kSmallPart[0];
-    if (parts > kSmallMaxParts) parts = kSmallMaxParts;
-    while (parts > 1 && units * parts > most_units) --parts;
-    if (parts < 1) parts = 1;
-    int size = (int)((longest + parts - 1) / parts + 7) / 8 * 8;
-    return size < 8 ? 8 : size;
+// A launch of attention under masks by units of 16 or 32 columns: which rows there are and how long they are, longest first.
+struct MaskRows {
+    struct {
+        int pages, units;                         // of the walk; units (groups x kv heads) of so many
+        bool cut;                                 // may come in parts
+    } row[PKV_MAX_SEQS];
+    int n = 0, longest = 0;
+    void add(int pages, int units, bool cut) {
+        row[n].pages = pages;
+        row[n].units = units;
+        row[n++].cut = cut;
+        if (pages > longest) longest = pages;
+    }
+};
+
+// What such a launch takes, in us, where rows longer than `part` pages come in parts of equal length.  A work-group takes tau us for a step of eight pages when
+// it is alone on its CU and memory keeps up.  The CUs get equal shares of the memory, whatever runs on them, and work-group i + 256 comes to the CU
+// of work-group i: 288 equal work-groups take 1.2 times what 256 or 432 of the same length in all take (144 rows of 354 pages, 1 kv head, in one, two and
+// three parts 68.3, 83.5, 66.5 us).  So the CUs' loads are added up in launch order, and run down together: with n of them left a step takes each of
+// them tau or n times the memory's time for its bytes.  Parts cost their join, work-groups beyond the places on the chip a start of their own.
+// The figures are fitted to 6200 launches (900 random calls, 24 to 1000 pages a part): the choice takes 2.5 % more than the best of all in the geometric mean,
+// one in twenty 11 % or more; cut into 512 shares' worth of pages 8.8 % and 30 %, never cut 20 % and 71 %.
+static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int part) {
+    constexpr int kPlaces = 768;
+    const double tau = two_tiles ? (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.27 : 0.72) : (m.D == 128 ? 1.09 : 0.83))
+                                 : (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.02 : 0.44) : (m.D == 128 ? 0.55 : 0.39));
+    const double step = (double)m.D * (m.dtype == PKV_BF16 ? 4 : 2) * 128 / 7.5e6;          // the memory's time for eight pages
+    auto with = [&](int n) {                      // what a step takes where n CUs are at work
+        const double shared = n * step, more = tau > shared ? tau : shared, x = (tau > shared ? shared : tau) / more;
+        return more * (1.0 + 0.19 * x * x * x * x);
+    };
+    double load[(int)kSmallCUs + 1] = {}, total = 0.0, longest = 0.0;
+    int most = 1;
+    int64_t wgs = 0, cut = 0;
+    for (int i = 0; i < rows.n; ++i) {
+        const int pages = rows.row[i].pages, parts = rows.row[i].cut && pages > part ? (pages + part - 1) / part : 1;
+        const double steps = (double)((pages + parts * 8 - 1) / (parts * 8));
+        const int64_t n = (int64_t)parts * rows.row[i].units;
+        most = most > parts ? most : parts;
+        longest = longest > steps ? longest : steps;
+        total += (double)n * steps;
+        for (int64_t k = wgs; k < wgs + n && k < kPlaces; ++k) load[k % kSmallCUs] += steps;
+        wgs += n;
+        if (parts > 1) cut += n;
+    }
+    double us = 5.4 + 4.3e-6 * (double)cut * cols * m.D;
+    if (wgs > kPlaces) us += total / kSmallCUs * with((int)kSmallCUs) + 0.5 * longest * tau;       // work-groups go where there is room
+    else
+        for (int i = 0; i < kSmallCUs; ++i)
+            if (load[i] != load[i + 1]) us += (load[i] - load[i + 1]) * with(i + 1);
+    if (wgs > kSmallWorkGroups) us += (two_tiles ? 0.72 : 0.06) * (double)(wgs - kSmallWorkGroups) / kSmallCUs;
+    if (most > 1) us += 0.96 + 0.12 * (most < 8 ? most : 8) + 0.14 * (most > 8 ? most - 8 : 0);
+    return us;
 }
+
+// Pages of a part: of some lengths the one that is estimated to be the best.
+static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, bool two_tiles) {
+    const int least = ((rows.longest + kSmallMaxParts - 1) / kSmallMaxParts + 7) / 8 * 8;
+    if (g_items > 0) {
+        double pages = 0.0;
+        for (int i = 0; i < rows.n; ++i) pages += (double)rows.row[i].pages * rows.row[i].units;
+        const int size = (int)(pages / g_items / 8.0 + 1.0) * 8;
+        return size < least ? least : (size < kMaskPart[0] ? kMaskPart[0] : size);
+    }
+    int best = rows.longest > 8 ? rows.longest : 8;
+    if (best <= kMaskPart[0]) return best;
+    double best_us = masked_us(m, rows, cols, two_tiles, best);
+    for (int part : kMaskPart) {
+        if (part >= rows.longest) break;
+        if (part < least) continue;
+        const double us = masked_us(m, rows, cols, two_tiles, part);
+        if (us < best_us) {
+            best_us = us;
+            best = part;
+        }
+    }
+    return best;
+}
+static MaskRows g_mask_rows;
 
 static MaskArgs mask_args(int window, int sinks) {
     MaskArgs mk{};
@@ -2533,13 +2606,16 @@ int decode_attention_window(int model, int batch, const void *q, const int32_t *
     AttnDesc d{};
     masked_desc(d, *m, batch, q, ctx_lens, out);
     const MaskArgs mk = mask_args(window, sinks);
-    int longest = 1;
-    for (int s = 0; s < batch; ++s) {
-        const int pages = masked_pages(m->row_len[s], mk.window, mk.sinks, 1);
-        longest = longest > pages ? longest : pages;
-    }
-    d.part_pages = masked_part_pages((int64_t)batch * m->Hkv, longest, (int64_t)(m->ws_floats / partial_floats(m->g, m->D)));
-    d.parts = (longest + d.part_pages - 1) / d.part_pages;
+    MaskRows &rows = g_mask_rows;
+    rows.n = rows.longest = 0;
+    for (int s = 0; s < batch; ++s) rows.add(masked_pages(m->row_len[s], mk.window, mk.sinks, 1), m->Hkv, true);
+    std::sort(rows.row, rows.row + rows.n, [](const auto &a, const auto &b) { return a.pages > b.pages; });
+    // partials: one per work-group, in the split-K workspace
+    const int64_t segs = (int64_t)batch * m->Hkv, slots = (int64_t)(m->ws_floats / partial_floats(m->g, m->D));
+    const int part = masked_part_pages(*m, rows, m->g, false);
+    d.parts = rows.longest > part ? (rows.longest + part - 1) / part : 1;
+    if (d.parts > 1 && segs * d.parts > slots) d.parts = slots / segs < 1 ? 1 : (int)(slots / segs);
+    d.part_pages = (part / 2 + 7) / 8 * 8;
     HIP_TRY(pkv_launch_window(d, mk, g_stream));
     return PKV_OK;
 }
@@ -2569,30 +2645,40 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
     MaskArgs mk = mask_args(window, sinks);
     mk.sees = sees;
     mk.words = words;
-    // Few columns a kv head: units of 16, whose four waves walk different pages; else groups of 128, whose waves walk the same pages with 32 each.
+    // Few columns a kv head: units of 16 or 32, whose four waves walk different pages; else groups of 128, whose waves walk the same pages with 32 each.
     int most = 0;
     for (int s = 0; s < batch; ++s) most = most > q_lens[s] ? most : q_lens[s];
-    const bool narrow = g_mask_form >= 0 ? g_mask_form == 0 && total <= 1 << 16 : most * m->g <= 16;
-    g_last_mask_form = narrow ? 0 : 1;
-    const int tile = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g, group = narrow ? 16 / m->g : PKV_PREFILL_WAVES * tile;
+    const int tile = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g;
+    int form = most * m->g <= 16 ? 0 : (most <= tile ? 2 : 1);
+    if (g_mask_form >= 0) form = total <= 1 << 16 ? g_mask_form : 1;
+    g_last_mask_form = form;
+    const int group = form == 0 ? 16 / m->g : (form == 2 ? tile : PKV_PREFILL_WAVES * tile);
     auto pages_of = [&](int s) { return masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < group ? q_lens[s] : group); };
     PlanBuilder plan(batch, PKV_PLAN_FEW);
-    if (narrow) {
-        int64_t groups = 0;
-        int longest = 1;
-        for (int s = 0; s < batch; ++s) {
-            groups += (q_lens[s] + group - 1) / group;
-            if (q_lens[s] > 0 && pages_of(s) > longest) longest = pages_of(s);
+    if (form != 1) {
+        d.cols = form == 0 ? 16 : 32;
+        // Partials of a launch's units, in the split-K workspace; arrivals are counted by sequence and kv head, so that only sequences of one group are cut.
+        const int64_t slots = (int64_t)(m->ws_floats / partial_floats(d.cols, m->D)) / m->Hkv;
+        auto groups_of = [&](int s) { return (q_lens[s] + group - 1) / group; };
+        for (int s0 = 0; s0 < batch;) {
+            const int s1 = s0 + plan.per_launch < batch ? s0 + plan.per_launch : batch;
+            MaskRows &rows = g_mask_rows;
+            rows.n = rows.longest = 0;
+            for (int s = s0; s < s1; ++s)
+                if (q_lens[s] > 0) rows.add(pages_of(s), groups_of(s) * m->Hkv, groups_of(s) == 1);
+            std::sort(rows.row, rows.row + rows.n, [](const auto &a, const auto &b) { return a.pages > b.pages; });
+            int part = masked_part_pages(*m, rows, (most < group ? most : group) * m->g, form == 2);
+            auto parts_of = [&](int s) { return groups_of(s) == 1 && pages_of(s) > part ? (pages_of(s) + part - 1) / part : 1; };
+            for (;; part += (part / 4 + 7) / 8 * 8) {
+                int64_t units = 0;
+                for (int s = s0; s < s1; ++s) units += (int64_t)groups_of(s) * parts_of(s);
+                if (units <= slots || part >= rows.longest) break;
+            }
+            d.part_pages = (part / 2 + 7) / 8 * 8;
+            for (int s = s0; s < s1; ++s) plan.add((uint32_t)q_lens[s], (uint32_t)(groups_of(s) * parts_of(s)), (uint32_t)parts_of(s), (uint32_t)(pages_of(s) / parts_of(s)));
+            HIP_TRY(pkv_launch_masked(d, mk, plan.take(s1), tree, g_stream));
+            s0 = s1;
         }
-        const int64_t slots = (int64_t)(m->ws_floats / partial_floats(16, m->D));
-        d.part_pages = masked_part_pages(groups * m->Hkv, longest, slots < (int64_t)m->cnt_cap ? slots : (int64_t)m->cnt_cap);
-        for (int s = 0; s < batch; ++s) {
-            if (plan.full()) HIP_TRY(pkv_launch_masked(d, mk, plan.take(s), tree, g_stream));
-            const int pages = pages_of(s), n = (q_lens[s] + group - 1) / group;
-            const int parts = pages > d.part_pages ? (pages + d.part_pages - 1) / d.part_pages : 1;
-            plan.add((uint32_t)q_lens[s], (uint32_t)(n * parts), (uint32_t)parts, (uint32_t)(pages / parts));
-        }
-        HIP_TRY(pkv_launch_masked(d, mk, plan.take(batch), tree, g_stream));
         return PKV_OK;
     }
     d.cols = tile * m->g;

@@ -8,7 +8,7 @@ namespace {
 // The decode step: a work-group per part of a (sequence, kv head).
 template <int D, int DT>
 __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_window_decode(const AttnDesc d, const MaskArgs mk) {
-    __shared__ __align__(16) float s_acc[SMALL_WAVES * 16 * 128];
+    __shared__ __align__(16) float s_acc[kMaskSums<1>];
     __shared__ float s_m[SMALL_WAVES * 16], s_l[SMALL_WAVES * 16];
     __shared__ uint32_t s_arrived;
     MaskUnit u;
@@ -32,18 +32,19 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_window_decode(const Att
     u.slot = u.seq * d.Hkv + u.kvh;
     u.step = partial_floats(d.g, D);
     u.partial = (size_t)u.slot * u.parts * u.step;
-    masked_part<D, DT, false>(d, mk, u, s_acc, s_m, s_l, nullptr, &s_arrived);
+    masked_part<D, DT, 1, false>(d, mk, u, s_acc, s_m, s_l, nullptr, &s_arrived);
 }
 
-// Chunks and drafted trees: a unit of the plan is a group of 16 / g query tokens, or one of the parts of what it sees.
-template <int D, int DT, bool TREE, int SEQS>
+// Chunks and drafted trees: a unit of the plan is a group of 16 NT / g query tokens, or one of the parts of what it sees.
+template <int D, int DT, int NT, bool TREE, int SEQS>
 __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d, const MaskArgs mk, const PlanOf<SEQS> plan) {
-    __shared__ __align__(16) float s_acc[SMALL_WAVES * 16 * 128];
-    __shared__ float s_m[SMALL_WAVES * 16], s_l[SMALL_WAVES * 16];
-    __shared__ uint32_t s_mask[TREE ? SMALL_WAVES * MASK_COLS * MASK_WORDS : 1];
+    constexpr int MC = kMaskCols<NT>;
+    __shared__ __align__(16) float s_acc[kMaskSums<NT>];
+    __shared__ float s_m[SMALL_WAVES * MC], s_l[SMALL_WAVES * MC];
+    __shared__ uint32_t s_mask[TREE ? SMALL_WAVES * MC * MASK_WORDS : 1];
     __shared__ uint32_t s_arrived;
     const PlanLanes<SEQS> lanes(plan);
-    const int unit = blockIdx.x / d.Hkv, size = MASK_COLS / d.g;
+    const int unit = blockIdx.x / d.Hkv, size = MC / d.g;
     const PlanUnit pu = lanes.find(plan, (uint32_t)unit);
     MaskUnit u;
     u.seq = pu.seq;
@@ -56,11 +57,11 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d
     u.chunk = pu.rows;
     u.tokens = pu.rows - u.chunk0 < size ? pu.rows - u.chunk0 : size;
     u.first = pu.row + u.chunk0;
-    u.slot = (unit - u.part) * d.Hkv + u.kvh;
-    const size_t floats = partial_floats(MASK_COLS, D);
-    u.partial = (size_t)u.slot * floats;
+    u.slot = u.seq * d.Hkv + u.kvh;                       // (a sequence that comes in parts has one group)
+    const size_t floats = partial_floats(MC, D);
+    u.partial = ((size_t)(unit - u.part) * d.Hkv + u.kvh) * floats;
     u.step = (size_t)d.Hkv * floats;
-    masked_part<D, DT, TREE>(d, mk, u, s_acc, s_m, s_l, s_mask, &s_arrived);
+    masked_part<D, DT, NT, TREE>(d, mk, u, s_acc, s_m, s_l, s_mask, &s_arrived);
 }
 
 // Groups of up to 128 columns (prefill_unit.h): a group of query tokens, four waves with 32 columns each, or one of the parts of what it sees.
@@ -152,16 +153,16 @@ void launch_wide(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan
     if (split_groups > 0) launch_merge(d, plan, split_groups, s);
 }
 
-template <bool TREE, int SEQS>
+template <int NT, bool TREE, int SEQS>
 void launch(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan, hipStream_t s) {
     static_assert(sizeof(AttnDesc) + sizeof(MaskArgs) + sizeof(plan) <= 4096, "a kernel's arguments end at 4 KB");
     const dim3 grid(plan.s[plan.n_seqs].unit * (unsigned)d.Hkv), wg(64 * SMALL_WAVES);
     if (d.dtype == PKV_BF16) {
-        if (d.D == 128) hipLaunchKernelGGL((k_masked<128, PKV_BF16, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
-        else hipLaunchKernelGGL((k_masked<64, PKV_BF16, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        if (d.D == 128) hipLaunchKernelGGL((k_masked<128, PKV_BF16, NT, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        else hipLaunchKernelGGL((k_masked<64, PKV_BF16, NT, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
     } else {
-        if (d.D == 128) hipLaunchKernelGGL((k_masked<128, PKV_E4M3, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
-        else hipLaunchKernelGGL((k_masked<64, PKV_E4M3, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        if (d.D == 128) hipLaunchKernelGGL((k_masked<128, PKV_E4M3, NT, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        else hipLaunchKernelGGL((k_masked<64, PKV_E4M3, NT, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
     }
 }
 
@@ -182,8 +183,13 @@ hipError_t pkv_launch_window(const AttnDesc &d, const MaskArgs &mk, hipStream_t 
 hipError_t pkv_launch_masked(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, hipStream_t s) {
     if (plan.s[plan.n_seqs].unit == 0) return hipSuccess;
     const auto few = few_of(plan);
-    if (tree) launch<true>(d, mk, few, s);
-    else launch<false>(d, mk, few, s);
+    if (d.cols <= 16) {
+        if (tree) launch<1, true>(d, mk, few, s);
+        else launch<1, false>(d, mk, few, s);
+    } else {
+        if (tree) launch<2, true>(d, mk, few, s);
+        else launch<2, false>(d, mk, few, s);
+    }
     return hipGetLastError();
 }
 

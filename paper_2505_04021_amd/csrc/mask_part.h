@@ -1,11 +1,11 @@
-// Attention under masks (mask_walk.h): the work-group that walks one part of a context for up to 16 columns (gfx950).
+// Attention under masks (mask_walk.h): the work-group that walks one part of a context for up to 16 or 32 columns (gfx950).
 #pragma once
 #include "decode_part.h"
 #include "mask_walk.h"
 
 namespace {
 
-// One work-group's part of a launch: up to 16 columns, `tokens` query tokens x the g heads of a kv head.
+// One work-group's part of a launch: its columns are `tokens` query tokens x the g heads of a kv head.
 struct MaskUnit {
     int seq, kvh, part, parts, size;     // which of how many parts of the walk, of how many pages
     int first, tokens;                   // rows of q and out
@@ -23,48 +23,65 @@ __device__ __forceinline__ void keep_v(u32x4 *v, uint32_t four) {
     for (int j = 0; j < Tile<D, DT>::NL; ++j) v[j] &= DT == PKV_BF16 ? mk4(m01, m23, m01, m23) : mk4(m, m, m, m);
 }
 
-constexpr int MASK_COLS = 16;                             // columns of a unit
+// Columns of a unit: one or two tiles of 16.
+template <int NT>
+constexpr int kMaskCols = 16 * NT;
+// LDS of a work-group: the sums of its four waves, or what the last one to arrive reads of all parts.
+template <int NT>
+constexpr int kMaskSums = SMALL_WAVES * 16 * NT * 128;
+static_assert(kMaskSums<1> >= 2 * MAX_PIECES * 16 && kMaskSums<2> >= 2 * MAX_PIECES * 32, "room for the maxima and denominators of all parts");
 
 // The work-group's four waves take the page pairs of its part in turn and join their sums through LDS; the last of several parts to arrive joins
 // those through memory (as attn_part in decode_part.h, whose comments say why it is built like this).
-template <int D, int DT, bool TREE>
+// With two tiles of columns a wave keeps one pair: K of the next pair is asked for when the scores have been taken, V when the products have, in the
+// registers that have become free.
+template <int D, int DT, int NT, bool TREE>
 __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &mk, const MaskUnit &u, float *s_acc, float *s_m, float *s_l, uint32_t *s_mask,
                                             uint32_t *s_arrived) {
     using TL = Tile<D, DT>;
+    constexpr int MC = kMaskCols<NT>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int G = lane >> 4, n = lane & 15, g = d.g, cols = u.tokens * g;
     const int32_t *row = d.table + (size_t)u.seq * d.row_stride;
-    const bool col_live = n < cols;
-    const int tok = col_live ? n / g : 0;
-    bf16x8 qf[TL::NK];
-    {
-        const uint16_t *qrow = d.q + ((size_t)(u.first + tok) * d.Hq + u.kvh * g + (col_live ? n - tok * g : 0)) * D;
+    bf16x8 qf[NT][TL::NK];
+    int tok[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const int col = 16 * c + n;
+        const bool live = col < cols;
+        tok[c] = live ? col / g : 0;
+        const uint16_t *qrow = d.q + ((size_t)(u.first + tok[c]) * d.Hq + u.kvh * g + (live ? col - tok[c] * g : 0)) * D;
 #pragma unroll
         for (int j = 0; j < TL::NK; ++j) {
             u32x4 v = mk4(0, 0, 0, 0);
-            if (col_live) v = *reinterpret_cast<const u32x4 *>(qrow + 8 * (4 * j + G));
-            qf[j] = *reinterpret_cast<bf16x8 *>(&v);
+            if (live) v = *reinterpret_cast<const u32x4 *>(qrow + 8 * (4 * j + G));
+            qf[c][j] = *reinterpret_cast<bf16x8 *>(&v);
         }
     }
     int ctx = PKV_CONST(int32_t, d.ctx_lens)[u.seq], cap = PKV_CONST(int32_t, d.row_len)[u.seq];
     asm volatile("" : "+s"(ctx), "+s"(cap));              // both at once
     cap *= PKV_T;
-    // what this lane's column sees, in tokens of the row
+    // what this lane's columns see, in tokens of the row
     const int window = mk.window;
-    int base = 0, hi, lo, L, lo_first, lo_last, hi_first;
-    uint32_t *mask_row = s_mask + (w * MASK_COLS + tok) * MASK_WORDS;
+    int base = 0, hi[NT], lo[NT], L, lo_first, lo_last, hi_first;
+    uint32_t *mask_row[NT];
     if constexpr (TREE) {
         base = ctx - u.chunk;
         L = base < 0 ? 0 : (ctx < cap ? ctx : cap);
-        const uint64_t *bits = mk.sees + (size_t)(u.first + tok) * mk.words;
-        const int seen = seen_drafts(bits, mk.words, u.chunk);
-        for (int i = 0; i < mk.words; ++i) {
-            const uint64_t x = bits[i];
-            mask_row[2 * i] = (uint32_t)x;
-            mask_row[2 * i + 1] = (uint32_t)(x >> 32);
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            // (a column that stands for no query has the first token's)
+            const uint64_t *bits = mk.sees + (size_t)(u.first + tok[c]) * mk.words;
+            const int seen = seen_drafts(bits, mk.words, u.chunk);
+            mask_row[c] = s_mask + (w * MC + tok[c]) * MASK_WORDS;
+            for (int i = 0; i < mk.words; ++i) {
+                const uint64_t x = bits[i];
+                mask_row[c][2 * i] = (uint32_t)x;
+                mask_row[c][2 * i + 1] = (uint32_t)(x >> 32);
+            }
+            hi[c] = base;
+            lo[c] = base + (seen > 0 ? seen : 1) - window;
         }
-        hi = base;
-        lo = base + (seen > 0 ? seen : 1) - window;
         lo_first = base + 1 - window;
         lo_last = base + u.chunk - window;
         hi_first = base;
@@ -72,32 +89,40 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
         L = ctx < 0 ? 0 : (ctx < cap ? ctx : cap);
         const int pos0 = L - u.chunk + u.chunk0;          // of the unit's first query
         L = pos0 + u.tokens;
-        hi = pos0 + tok + 1;
-        lo = hi - window;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            hi[c] = pos0 + tok[c] + 1;
+            lo[c] = hi[c] - window;
+        }
         lo_first = pos0 + 1 - window;
         lo_last = L - window;
         hi_first = pos0 + 1;
     }
     const Walk walk = walk_of(L, lo_first, lo_last, hi_first, mk.sinks);
     const int shift = walk.skip * PKV_T;
-    hi -= shift;
-    lo -= shift;
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        hi[c] -= shift;
+        lo[c] -= shift;
+    }
     base -= shift;
     const int n_pages = walk.pages(), max_parts = u.parts;
     constexpr int STEP = 2 * SMALL_WAVES;
-    int size = u.size;
-    if (n_pages > max_parts * size) {                     // longer than the host knew
-        size = (n_pages + max_parts - 1) / max_parts;
-        size = (size + STEP - 1) / STEP * STEP;
-    }
+    // as many parts of equal length as the host asked for, but none shorter than u.size
+    int size = (n_pages + max_parts - 1) / max_parts;
+    size = (size + STEP - 1) / STEP * STEP;
+    size = size < u.size ? u.size : size;
     const int n_parts = n_pages > size ? (n_pages + size - 1) / size : 1;
     if (u.part >= n_parts) return;
     const int page0 = u.part * size + 2 * w, pe = (u.part + 1) * size < n_pages ? (u.part + 1) * size : n_pages;
-    State<D, DT> st;
+    State<D, DT> st[NT];
 #pragma unroll
-    for (int jt = 0; jt < TL::NV; ++jt) st.acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st.m = -INFINITY;
-    st.l = 0.f;
+    for (int c = 0; c < NT; ++c) {
+#pragma unroll
+        for (int jt = 0; jt < TL::NV; ++jt) st[c].acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        st[c].m = -INFINITY;
+        st[c].l = 0.f;
+    }
 
     // This wave's pairs: pages page0 + STEP k and the one behind it.  Lane i works out where page i & 1 of pair window + (i >> 1) is.
     bool bad = false;
@@ -134,85 +159,154 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
         for (int j = 0; j < TL::NL; ++j) r[j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff + j * 1024, at, 2 /* non-temporal */);
         asm volatile("" ::: "memory");                    // in this order everywhere: loads in flight are counted
     };
-    auto load_pair = [&](PairRegs<D, DT> &r, int k) __attribute__((always_inline)) {
-        const __amdgpu_buffer_rsrc_t a = tiles(k, 0), b = tiles(k, 1);
-        load(r.a.k, a, 0);
-        load(r.a.v, a, TL::TILE_BYTES);
-        load(r.b.k, b, 0);
-        load(r.b.v, b, TL::TILE_BYTES);
-        if (DT == PKV_E4M3) {
-            const int at = 2 * (k - pair0);
-            r.a.sk = __uint_as_float(lane_of(__float_as_uint(page_sk), at));
-            r.a.sv = __uint_as_float(lane_of(__float_as_uint(page_sv), at));
-            r.b.sk = __uint_as_float(lane_of(__float_as_uint(page_sk), at + 1));
-            r.b.sv = __uint_as_float(lane_of(__float_as_uint(page_sv), at + 1));
-        }
-    };
-    auto step = [&](PairRegs<D, DT> &r, PairRegs<D, DT> &o, int k, bool more) __attribute__((always_inline)) {
-        if (more) load_pair(o, k + 1);
-        const int p = page0 + STEP * k, x0 = PKV_T * p;
-        // (Decided ahead of the products, and without branches: the compiler waits for a product's result along one of two ways that part behind it and
-        // meet where it is read, and not along the other.)
-        const bool second = p + 1 < pe, masked = !walk.plain(x0) | !second;
+    auto scale_of = [&](float x, int k, int half) __attribute__((always_inline)) { return __uint_as_float(lane_of(__float_as_uint(x), 2 * (k - pair0) + half)); };
+    // Scores of pair k's 32 tokens, scaled and masked, as the columns' softmax takes them; `r`'s V is blanked where no query sees it.
+    // (Whether masks are needed is decided ahead of the products, and without branches: the compiler waits for a product's result along one of two
+    // ways that part behind it and meet where it is read, and not along the other.)
+    auto scores = [&](float (*s)[8], const PairRegs<D, DT> &r) __attribute__((always_inline)) {
         const float sca = DT == PKV_E4M3 ? d.scale_log2 * r.a.sk : d.scale_log2, scb = DT == PKV_E4M3 ? d.scale_log2 * r.b.sk : d.scale_log2;
-        const f32x4 sa = qk_page<D, DT>(r.a, qf), sb = qk_page<D, DT>(r.b, qf);
-        float s[8];
+        f32x4 sa[NT], sb[NT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[i] = sa[i] * sca;
-            s[4 + i] = sb[i] * scb;
+        for (int c = 0; c < NT; ++c) {
+            sa[c] = qk_page<D, DT>(r.a, qf[c]);
+            sb[c] = qk_page<D, DT>(r.b, qf[c]);
         }
-        // pairs with tokens that not every column sees: a branch of its own
-        if (masked) {
-            const uint32_t there = below(walk.len - x0) & (second ? 0xffffffffu : 0xffffu);
-            uint32_t mine = seen_bits(x0, hi, lo, walk.sinks);
-            if constexpr (TREE) mine |= row_bits(mask_row, 2 * mk.words, x0 - base);
-            mine = (mine & there) >> (4 * G);
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[c][i] = sa[c][i] * sca;
+                s[c][4 + i] = sb[c][i] * scb;
+            }
+    };
+    auto pair_is_masked = [&](int k) __attribute__((always_inline)) {
+        const int p = page0 + STEP * k;
+        return !walk.plain(PKV_T * p) | !(p + 1 < pe);
+    };
+    auto there = [&](int k) __attribute__((always_inline)) {          // tokens of pair k that are in the part
+        const int p = page0 + STEP * k;
+        return below(walk.len - PKV_T * p) & (p + 1 < pe ? 0xffffffffu : 0xffffu);
+    };
+    auto mask_scores = [&](float (*s)[8], int k) __attribute__((always_inline)) {
+        const int x0 = PKV_T * (page0 + STEP * k);
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            uint32_t mine = seen_bits(x0, hi[c], lo[c], walk.sinks);
+            if constexpr (TREE) mine |= row_bits(mask_row[c], 2 * mk.words, x0 - base);
+            mine = (mine & there(k)) >> (4 * G);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                  // (a select, so that a NaN logit of an unseen token cannot leak)
-                if (!(mine >> i & 1u)) s[i] = -INFINITY;
-                if (!(mine >> (16 + i) & 1u)) s[4 + i] = -INFINITY;
+                if (!(mine >> i & 1u)) s[c][i] = -INFINITY;
+                if (!(mine >> (16 + i) & 1u)) s[c][4 + i] = -INFINITY;
             }
-            const uint32_t any = (there & walk.some(x0)) >> (4 * G);
-            keep_v<D, DT>(r.a.v, any);
-            keep_v<D, DT>(r.b.v, any >> 16);
         }
-        bf16x8 phv, plv;
-        softmax_pair<D, DT>(st, s, r.a.sv, r.b.sv, phv, plv);
+    };
+    auto mask_v = [&](PairRegs<D, DT> &r, int k) __attribute__((always_inline)) {
+        const uint32_t any = (there(k) & walk.some(PKV_T * (page0 + STEP * k))) >> (4 * G);
+        keep_v<D, DT>(r.a.v, any);
+        keep_v<D, DT>(r.b.v, any >> 16);
+    };
+    auto products = [&](const PairRegs<D, DT> &r, const bf16x8 *ph, const bf16x8 *pl) __attribute__((always_inline)) {
 #pragma unroll
         for (int jt = 0; jt < TL::NV; ++jt) {
             const u32x2 va = v_half<D, DT>(r.a, jt), vb = v_half<D, DT>(r.b, jt);
             const bf16x8 av = as_bf16x8(mk4(va.x, va.y, vb.x, vb.y));
-            st.acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, phv, st.acc[jt], 0, 0, 0);
-            st.acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, plv, st.acc[jt], 0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                st[c].acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, ph[c], st[c].acc[jt], 0, 0, 0);
+                st[c].acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pl[c], st[c].acc[jt], 0, 0, 0);
+            }
         }
     };
     const int n_pairs = page0 < pe ? (pe - page0 + STEP - 1) / STEP : 0;
-    if (n_pairs > 0) {
-        PairRegs<D, DT> ring[2];
-        locate(0);
-        load_pair(ring[0], 0);
-        int k = 0;
-        if (n_pairs > 1) {
-            do {
-                if (k + 2 - pair0 >= 32) locate(k + 1);
-                step(ring[0], ring[1], k, true);
-                step(ring[1], ring[0], k + 1, true);
-                k += 2;
-            } while (k + 2 <= n_pairs);
+    if constexpr (NT == 1) {
+        auto load_pair = [&](PairRegs<D, DT> &r, int k) __attribute__((always_inline)) {
+            const __amdgpu_buffer_rsrc_t a = tiles(k, 0), b = tiles(k, 1);
+            load(r.a.k, a, 0);
+            load(r.a.v, a, TL::TILE_BYTES);
+            load(r.b.k, b, 0);
+            load(r.b.v, b, TL::TILE_BYTES);
+            if (DT == PKV_E4M3) {
+                r.a.sk = scale_of(page_sk, k, 0);
+                r.a.sv = scale_of(page_sv, k, 0);
+                r.b.sk = scale_of(page_sk, k, 1);
+                r.b.sv = scale_of(page_sv, k, 1);
+            }
+        };
+        auto step = [&](PairRegs<D, DT> &r, PairRegs<D, DT> &o, int k, bool more) __attribute__((always_inline)) {
+            if (more) load_pair(o, k + 1);
+            const bool masked = pair_is_masked(k);
+            float s[NT][8];
+            scores(s, r);
+            if (masked) {                                 // a branch of its own
+                mask_scores(s, k);
+                mask_v(r, k);
+            }
+            bf16x8 ph[NT], pl[NT];
+            softmax_pair<D, DT>(st[0], s[0], r.a.sv, r.b.sv, ph[0], pl[0]);
+            products(r, ph, pl);
+        };
+        if (n_pairs > 0) {
+            PairRegs<D, DT> ring[2];
+            locate(0);
+            load_pair(ring[0], 0);
+            int k = 0;
+            if (n_pairs > 1) {
+                do {
+                    if (k + 2 - pair0 >= 32) locate(k + 1);
+                    step(ring[0], ring[1], k, true);
+                    step(ring[1], ring[0], k + 1, true);
+                    k += 2;
+                } while (k + 2 <= n_pairs);
+            }
+            if (k < n_pairs) step(ring[0], ring[1], k, false);
         }
-        if (k < n_pairs) step(ring[0], ring[1], k, false);
-    }
-    float l = st.l;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (n < cols) {
-        float *a = s_acc + (w * cols + n) * D;
+    } else if (n_pairs > 0) {
+        PairRegs<D, DT> r;
+        auto load_k = [&](int k) __attribute__((always_inline)) {
+            load(r.a.k, tiles(k, 0), 0);
+            load(r.b.k, tiles(k, 1), 0);
+            r.a.sk = DT == PKV_E4M3 ? scale_of(page_sk, k, 0) : 0.f;
+            r.b.sk = DT == PKV_E4M3 ? scale_of(page_sk, k, 1) : 0.f;
+        };
+        auto load_v = [&](int k) __attribute__((always_inline)) {
+            load(r.a.v, tiles(k, 0), TL::TILE_BYTES);
+            load(r.b.v, tiles(k, 1), TL::TILE_BYTES);
+            r.a.sv = DT == PKV_E4M3 ? scale_of(page_sv, k, 0) : 0.f;
+            r.b.sv = DT == PKV_E4M3 ? scale_of(page_sv, k, 1) : 0.f;
+        };
+        locate(0);
+        load_k(0);
+        load_v(0);
+        for (int k = 0; k < n_pairs; ++k) {
+            if (k + 1 - pair0 >= 32) locate(k + 1);
+            const bool masked = pair_is_masked(k);
+            float s[NT][8];
+            scores(s, r);
+            load_k(k + 1);                                // (a pair behind the part's last has no records: nothing is read)
+            if (masked) mask_scores(s, k);
+            bf16x8 ph[NT], pl[NT];
 #pragma unroll
-        for (int jt = 0; jt < TL::NV; ++jt) *reinterpret_cast<f32x4 *>(a + 16 * jt + 4 * G) = st.acc[jt];
-        if (G == 0) {
-            s_m[w * 16 + n] = st.m;
-            s_l[w * 16 + n] = l;
+            for (int c = 0; c < NT; ++c) softmax_pair<D, DT>(st[c], s[c], r.a.sv, r.b.sv, ph[c], pl[c]);
+            if (masked) mask_v(r, k);
+            products(r, ph, pl);
+            load_v(k + 1);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        float l = st[c].l;
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        const int col = 16 * c + n;
+        if (col < cols) {
+            float *a = s_acc + (w * cols + col) * D;
+#pragma unroll
+            for (int jt = 0; jt < TL::NV; ++jt) *reinterpret_cast<f32x4 *>(a + 16 * jt + 4 * G) = st[c].acc[jt];
+            if (G == 0) {
+                s_m[w * MC + col] = st[c].m;
+                s_l[w * MC + col] = l;
+            }
         }
     }
     if (__any(bad) && lane == 0) atomicOr(d.err, 1u);
@@ -226,13 +320,13 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
         const int c = i / (D / 4), x = i - c * (D / 4), t = c / g;
         float M = s_m[c];
 #pragma unroll
-        for (int v = 1; v < SMALL_WAVES; ++v) M = fmaxf(M, s_m[v * 16 + c]);
+        for (int v = 1; v < SMALL_WAVES; ++v) M = fmaxf(M, s_m[v * MC + c]);
         float den = 0.f;
         f32x4 num = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < SMALL_WAVES; ++v) {
-            const float f = merge_weight(s_m[v * 16 + c], M);
-            den += f * s_l[v * 16 + c];
+            const float f = merge_weight(s_m[v * MC + c], M);
+            den += f * s_l[v * MC + c];
             num += f * *reinterpret_cast<const f32x4 *>(s_acc + (v * cols + c) * D + 4 * x);
         }
         if (whole) {
@@ -267,7 +361,7 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
     for (int i = threadIdx.x; i < n_parts * cols; i += 64 * SMALL_WAVES) {
         const int p = i / cols, c = i - p * cols;
         s_acc[i] = first[(size_t)p * u.step + cols * D + c];
-        s_acc[MAX_PIECES * 16 + i] = first[(size_t)p * u.step + cols * D + cols + c];
+        s_acc[MAX_PIECES * MC + i] = first[(size_t)p * u.step + cols * D + cols + c];
     }
     __syncthreads();
     for (int i = threadIdx.x; i < quads; i += 64 * SMALL_WAVES) {
@@ -281,7 +375,7 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
             for (int k = 0; k < 8; ++k)
                 if (p0 + k < n_parts) {
                     const float f = merge_weight(s_acc[(p0 + k) * cols + c], M);
-                    den += f * s_acc[MAX_PIECES * 16 + (p0 + k) * cols + c];
+                    den += f * s_acc[MAX_PIECES * MC + (p0 + k) * cols + c];
                     num += f * v[k];
                 }
         }

@@ -13,9 +13,9 @@ pytestmark = pytest.mark.gpu
 WINDOWS = [(1, 0), (1, 1), (16, 0), (17, 4), (5, 40), (100, 4), (64, 16), (130, 33), (1000, 0), (1 << 30, 3), (2147483647, 2147483647)]
 
 
-@pytest.fixture(params=[0, 1], ids=["units of 16", "groups of 128"])
+@pytest.fixture(params=[0, 1, 2], ids=["units of 16", "groups of 128", "units of 32"])
 def form(gpu, request):  # noqa: F811
-    """Both ways in which chunks and trees fall into work-groups."""
+    """The ways in which chunks and trees fall into work-groups."""
     assert gpu.set_mask_form(request.param) == 0
     yield request.param
     gpu.set_mask_form(-1)
