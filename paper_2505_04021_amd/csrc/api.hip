@@ -2586,6 +2586,52 @@ static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, boo
     }
     return best;
 }
+// The same for groups of 128 columns and parts of `pairs` page pairs (0: uncut).  A work-group takes t1 us a pair by itself and t2 a pair beside another one on its CU, and
+// every one takes kGroupPairs pairs besides its own; beyond two to a CU they go where there is room.  Parts' sums are written and read once, and joined by a launch of
+// their own.  Fitted to 3100 launches (350 random calls): the choice takes 1.7 % more than the best, one in twenty 7.6 % or more (prefill_part_pairs 2.7 and 13.2).
+static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs) {
+    const bool bf16 = m.dtype == PKV_BF16, wide = m.D == 128;
+    const double t1 = wide ? (bf16 ? 0.60 : 0.70) : (bf16 ? 0.42 : 0.52), t2 = wide ? (bf16 ? 0.40 : 0.49) : (bf16 ? 0.28 : 0.34);
+    constexpr double kGroupPairs = 5.7;
+    double load[2][(int)kSmallCUs] = {}, total = 0.0, longest = 0.0;
+    int64_t wgs = 0, cut = 0;
+    for (int i = 0; i < rows.n; ++i) {
+        const int all = (rows.row[i].pages + 1) / 2, parts = prefill_parts(rows.row[i].pages, pairs);
+        const double len = (all + parts - 1) / parts + kGroupPairs;
+        const int64_t n = (int64_t)parts * rows.row[i].units;
+        longest = longest > len ? longest : len;
+        total += (double)n * len;
+        for (int64_t k = wgs; k < wgs + n && k < kSmallWorkGroups; ++k) load[k / kSmallCUs][k % kSmallCUs] = len;
+        wgs += n;
+        if (parts > 1) cut += n;
+    }
+    double us = longest * t1;
+    if (wgs > kSmallWorkGroups) {
+        const double even = total / kSmallCUs * t2 + 0.585 * us;
+        us = even > us ? even : us;
+    } else if (wgs > kSmallCUs) {
+        for (int i = 0; i < kSmallCUs; ++i) {
+            const double a = load[0][i], b = load[1][i], both = 2.0 * (a < b ? a : b) * t2 + fabs(a - b) * t1;
+            us = us > both ? us : both;
+        }
+    }
+    if (cut > 0) us += 4.4 + 1.2e-6 * (double)cut * PKV_PREFILL_COLS * (m.D + 4);
+    return us;
+}
+
+static double masked_part_pairs(const Model &m, const MaskRows &rows) {
+    if (g_items > 0) return (double)g_items;
+    double best = 0.0, best_us = masked_wide_us(m, rows, 0.0);
+    for (int pages : kMaskPart) {
+        if (pages >= rows.longest) break;
+        const double us = masked_wide_us(m, rows, pages * 0.5);
+        if (us < best_us) {
+            best_us = us;
+            best = pages * 0.5;
+        }
+    }
+    return best;
+}
 static MaskRows g_mask_rows;
 
 static MaskArgs mask_args(int window, int sinks) {
@@ -2698,8 +2744,14 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
             const int rc = launch(plan.take(s));
             if (rc) return rc;
         }
-        if (s % plan.per_launch == 0)
-            part_pairs = prefill_part_pairs(*m, s, s + plan.per_launch < batch ? s + plan.per_launch : batch, q_lens, group, pages_of);
+        if (s % plan.per_launch == 0) {
+            MaskRows &rows = g_mask_rows;
+            rows.n = rows.longest = 0;
+            for (int i = s; i < s + plan.per_launch && i < batch; ++i)
+                if (q_lens[i] > 0) rows.add(pages_of(i), (q_lens[i] + group - 1) / group * m->Hkv, true);
+            std::sort(rows.row, rows.row + rows.n, [](const auto &x, const auto &y) { return x.pages > y.pages; });
+            part_pairs = masked_part_pairs(*m, rows);
+        }
         const int parts = prefill_parts(pages_of(s), part_pairs), groups = (q_lens[s] + group - 1) / group;
         plan.add((uint32_t)q_lens[s], (uint32_t)(groups * parts), (uint32_t)parts, (uint32_t)(pages_of(s) / parts));
         if (parts > 1 && groups > split_groups) split_groups = groups;

@@ -101,8 +101,22 @@ struct MaskedGroup {
     __device__ __forceinline__ int sees(const AttnDesc &) const { return walk.len; }
     __device__ __forceinline__ bool partial() const { return parts > 1; }
     __device__ __forceinline__ size_t tile(const AttnDesc &d, int kvh, int w) const { return ((size_t)slot * d.Hkv + kvh) * PF_WAVES + w; }
-    // tokens at the walk's end that none of the group's queries sees but the last k
-    __device__ __forceinline__ int behind(int k) const { return TREE ? 0 : k; }
+    // of queries i .. i + n - 1, along the walk: where their windows begin, first and last, below which token all see all but for the windows, and below which some do
+    __device__ __forceinline__ void tile_range(int i, int n, int &lo_min, int &lo_max, int &hi_min, int &hi_max) const {
+        if constexpr (TREE) {
+            lo_min = walk.lo_min;
+            lo_max = walk.lo_max;
+            hi_min = walk.hi_min;
+            hi_max = n > 0 ? walk.len : 0;
+        } else {
+            const int shift = walk.skip * PKV_T, last = pos0 + i + n - shift;        // (behind the last one)
+            auto within = [&](int x) __attribute__((always_inline)) { return x < 0 ? 0 : (x < walk.len ? x : walk.len); };
+            lo_min = within(last - n + 1 - mk.window);
+            lo_max = within(last - mk.window);
+            hi_min = within(last - n + 1);
+            hi_max = n > 0 ? within(last) : 0;
+        }
+    }
     // what query i sees, token t of wave w's tile: sinks, tokens from `from` on below `upto`, and those of the row that is returned
     __device__ __forceinline__ uint32_t *column(int w, int t, int i, int &from, int &upto) const {
         if constexpr (TREE) {

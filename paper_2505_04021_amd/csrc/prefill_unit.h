@@ -123,15 +123,19 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     const int col_lim = at_least(UNIT::CAUSAL && col_live ? L - (ntok - 1 - (t0 + tok)) : L);        // tokens this column sees
     int tile_lim = my_tok > 0 ? at_least(L - (UNIT::CAUSAL ? ntok - t0 - my_tok : 0)) : 0;     // tokens some column of the tile sees
     // MASKED: this lane's column sees sinks and tokens from `from` on below `upto`, and those of its row of a mask
-    int from = 0, upto = 0;
+    int from = 0, upto = 0, p_gap = 0, p_sinks = 0;
     uint32_t *mask_row = nullptr;
     if constexpr (UNIT::MASKED) {
         // (a column that stands for no query has the tile's first token's, or, in a tile without any, the unit's last one's)
         const int t = col_live ? tok : 0, i = t0 + t;
         mask_row = u.column(w, t, i < ntok ? i : ntok - 1, from, upto);
-        p_first = (u.walk.lo_max + 31) >> 5;
-        p_plain = u.walk.hi_min >> 5;
-        tile_lim = my_tok > 0 ? L - u.behind(ntok - t0 - my_tok) : 0;
+        // of this wave's tile: pairs that need masks, and those that it need not take at all
+        int lo_min, lo_max, hi_min;
+        u.tile_range(t0, my_tok, lo_min, lo_max, hi_min, tile_lim);
+        p_first = (lo_max + 31) >> 5;
+        p_plain = hi_min >> 5;
+        p_gap = lo_min >> 5;
+        p_sinks = (u.walk.sinks + 31) >> 5;
     }
     auto seen = [&](int p) __attribute__((always_inline)) {           // of pair p, from this lane's first token on
         if constexpr (UNIT::MASKED) return u.seen(32 * p, from, upto, mask_row) >> (4 * h);
@@ -312,6 +316,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             }
     };
 
+    auto takes = [&](int p) __attribute__((always_inline)) { return UNIT::MASKED ? (p >= p_gap) | (p < p_sinks) : true; };
     auto needs_mask = [&](int p) __attribute__((always_inline)) { return UNIT::MASKED ? (p < p_first) | (p >= p_plain) : p >= p_plain; };
     // ---- one pair's softmax, in two parts.  Arguments: t = score * scale - m (log2 domain) against the reference
     // point m as it stands.  m need not be the column's maximum, only near it: it moves, and the sums are
@@ -499,7 +504,8 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
         };
         auto step = [&]() __attribute__((always_inline)) {
             const int p = p_begin + r;
-            const bool now = 32 * p < tile_lim, next = (r + 1 < np) & (32 * (p + 1) < tile_lim);     // (neither where no token is the wave's)
+            // (neither where no token is the wave's)
+            const bool now = (32 * p < tile_lim) & takes(p), next = (r + 1 < np) & (32 * (p + 1) < tile_lim) & takes(p + 1);
             if (now) {
                 read_v(r);
                 probabilities();
@@ -509,7 +515,7 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
                 scores();
             }
             if (r + 1 < np && !(r & (MEET - 1))) meet(r);
-            if (next && r + 2 < np) read_k(r + 2);
+            if ((UNIT::MASKED ? live : next) && r + 2 < np) read_k(r + 2);       // (under masks a pair that is taken may follow one that is not)
             if (now) {
                 if (UNIT::MASKED ? needs_mask(p) : 32 * (p + 1) > L) blank_v(p);
                 accumulate(ph);
