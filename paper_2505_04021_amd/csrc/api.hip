@@ -1313,7 +1313,7 @@ int model_register_layers(int pool, int q_heads, int kv_heads, int head_dim, int
     // priming launch)
     {
         const size_t decode = ws_floats_for(m, kDefaultItems, m.g), masked = (size_t)kMaskPartials * partial_floats(32, m.D);
-        const int rc = ensure_workspace(m, decode > masked ? decode : masked, (size_t)max_seqs * kv_heads, 1);
+        const int rc = ensure_workspace(m, decode > masked ? decode : masked, (size_t)PKV_MASK_GROUPS * max_seqs * kv_heads, 1);
         if (rc) {
             free_model_dev(m);
             return rc;
@@ -2489,7 +2489,6 @@ int decode_attention_prefix(int model, int batch, const void *q, const int32_t *
 
 /* ------------------------------------------------ windows and drafted trees */
 
-
 // Pages that the last query of a sequence walks, as far as the host knows.
 static int masked_pages(int pages, int window, int sinks, int queries) {
     const int64_t most = (int64_t)(sinks + 15) / 16 + ((int64_t)window + queries + 15) / 16 + 1;
@@ -2530,7 +2529,7 @@ struct MaskRows {
 // them tau or n times the memory's time for its bytes.  Parts cost their join, work-groups beyond the places on the chip a start of their own.
 // The figures are fitted to 6200 launches (900 random calls, 24 to 1000 pages a part): the choice takes 2.5 % more than the best of all in the geometric mean,
 // one in twenty 11 % or more; cut into 512 shares' worth of pages 8.8 % and 30 %, never cut 20 % and 71 %.
-static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int part) {
+static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int part, int64_t slots) {
     constexpr int kPlaces = 768;
     const double tau = two_tiles ? (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.27 : 0.72) : (m.D == 128 ? 1.09 : 0.83))
                                  : (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.02 : 0.44) : (m.D == 128 ? 0.55 : 0.39));
@@ -2553,6 +2552,7 @@ static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two
         wgs += n;
         if (parts > 1) cut += n;
     }
+    if (most > 1 && wgs > slots) return 1e30;
     double us = 5.4 + 4.3e-6 * (double)cut * cols * m.D;
     if (wgs > kPlaces) us += total / kSmallCUs * with((int)kSmallCUs) + 0.5 * longest * tau;       // work-groups go where there is room
     else
@@ -2563,8 +2563,8 @@ static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two
     return us;
 }
 
-// Pages of a part: of some lengths the one that is estimated to be the best.
-static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, bool two_tiles) {
+// Pages of a part: of some lengths the one that is estimated to be the best.  `slots`: work-groups whose partials the workspace takes.
+static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int64_t slots, double *estimate = nullptr) {
     const int least = ((rows.longest + kSmallMaxParts - 1) / kSmallMaxParts + 7) / 8 * 8;
     if (g_items > 0) {
         double pages = 0.0;
@@ -2573,19 +2573,21 @@ static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, boo
         return size < least ? least : (size < kMaskPart[0] ? kMaskPart[0] : size);
     }
     int best = rows.longest > 8 ? rows.longest : 8;
-    if (best <= kMaskPart[0]) return best;
-    double best_us = masked_us(m, rows, cols, two_tiles, best);
+    if (best <= kMaskPart[0] && !estimate) return best;
+    double best_us = masked_us(m, rows, cols, two_tiles, best, slots);
     for (int part : kMaskPart) {
         if (part >= rows.longest) break;
         if (part < least) continue;
-        const double us = masked_us(m, rows, cols, two_tiles, part);
+        const double us = masked_us(m, rows, cols, two_tiles, part, slots);
         if (us < best_us) {
             best_us = us;
             best = part;
         }
     }
+    if (estimate) *estimate = best_us;
     return best;
 }
+
 // The same for groups of 128 columns and parts of `pairs` page pairs (0: uncut).  A work-group takes t1 us a pair by itself and t2 a pair beside another one on its CU, and
 // every one takes kGroupPairs pairs besides its own; beyond two to a CU they go where there is room.  Parts' sums are written and read once, and joined by a launch of
 // their own.  Fitted to 3100 launches (350 random calls): the choice takes 1.7 % more than the best, one in twenty 7.6 % or more (prefill_part_pairs 2.7 and 13.2).
@@ -2593,9 +2595,10 @@ static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs)
     const bool bf16 = m.dtype == PKV_BF16, wide = m.D == 128;
     const double t1 = wide ? (bf16 ? 0.60 : 0.70) : (bf16 ? 0.42 : 0.52), t2 = wide ? (bf16 ? 0.40 : 0.49) : (bf16 ? 0.28 : 0.34);
     constexpr double kGroupPairs = 5.7;
-    double load[2][(int)kSmallCUs] = {}, total = 0.0, longest = 0.0;
+    double load[2][(int)kSmallCUs] = {}, total = 0.0, longest = 0.0, bytes = 0.0;
     int64_t wgs = 0, cut = 0;
     for (int i = 0; i < rows.n; ++i) {
+        bytes += (double)rows.row[i].units * rows.row[i].pages * (m.D * (bf16 ? 64 : 32));
         const int all = (rows.row[i].pages + 1) / 2, parts = prefill_parts(rows.row[i].pages, pairs);
         const double len = (all + parts - 1) / parts + kGroupPairs;
         const int64_t n = (int64_t)parts * rows.row[i].units;
@@ -2615,11 +2618,13 @@ static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs)
             us = us > both ? us : both;
         }
     }
+    const double memory = bytes / 6.8e6, more = us > memory ? us : memory, x = (us > memory ? memory : us) / (more > 0.0 ? more : 1.0);
+    us = 5.3 + more * (1.0 + 0.19 * x * x * x * x);
     if (cut > 0) us += 4.4 + 1.2e-6 * (double)cut * PKV_PREFILL_COLS * (m.D + 4);
     return us;
 }
 
-static double masked_part_pairs(const Model &m, const MaskRows &rows) {
+static double masked_part_pairs(const Model &m, const MaskRows &rows, double *estimate = nullptr) {
     if (g_items > 0) return (double)g_items;
     double best = 0.0, best_us = masked_wide_us(m, rows, 0.0);
     for (int pages : kMaskPart) {
@@ -2630,8 +2635,10 @@ static double masked_part_pairs(const Model &m, const MaskRows &rows) {
             best = pages * 0.5;
         }
     }
+    if (estimate) *estimate = best_us;
     return best;
 }
+
 static MaskRows g_mask_rows;
 
 static MaskArgs mask_args(int window, int sinks) {
@@ -2658,7 +2665,7 @@ int decode_attention_window(int model, int batch, const void *q, const int32_t *
     std::sort(rows.row, rows.row + rows.n, [](const auto &a, const auto &b) { return a.pages > b.pages; });
     // partials: one per work-group, in the split-K workspace
     const int64_t segs = (int64_t)batch * m->Hkv, slots = (int64_t)(m->ws_floats / partial_floats(m->g, m->D));
-    const int part = masked_part_pages(*m, rows, m->g, false);
+    const int part = masked_part_pages(*m, rows, m->g, false, slots);
     d.parts = rows.longest > part ? (rows.longest + part - 1) / part : 1;
     if (d.parts > 1 && segs * d.parts > slots) d.parts = slots / segs < 1 ? 1 : (int)(slots / segs);
     d.part_pages = (part / 2 + 7) / 8 * 8;
@@ -2691,11 +2698,28 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
     MaskArgs mk = mask_args(window, sinks);
     mk.sees = sees;
     mk.words = words;
-    // Few columns a kv head: units of 16 or 32, whose four waves walk different pages; else groups of 128, whose waves walk the same pages with 32 each.
+    // Few columns a kv head: units of 16 or 32, whose four waves walk different pages; many: groups of 128, whose waves walk the same pages with 32 each.  Between,
+    // what either is estimated to take decides: units of 32 want no join launch and start sooner, but every 32 columns read the context for themselves.  Us, units
+    // of 32 and groups: 40 columns of 16/8/128 e4m3, 16 x 500 tokens 15.4, 22.4; 64 columns, 64 x 3125 tokens of 16/4/128 bf16 182, 115; 96, 4 x 4000 of 4/4/128 24.5, 25.2.
     int most = 0;
     for (int s = 0; s < batch; ++s) most = most > q_lens[s] ? most : q_lens[s];
     const int tile = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g;
     int form = most * m->g <= 16 ? 0 : (most <= tile ? 2 : 1);
+    if (form == 1 && most <= PKV_MASK_GROUPS * tile) {
+        MaskRows &rows = g_mask_rows;
+        double units = 0.0, groups = 0.0;
+        for (int f : {2, 1}) {
+            const int size = f == 2 ? tile : PKV_PREFILL_WAVES * tile;
+            rows.n = rows.longest = 0;
+            for (int s = 0; s < batch && s < PKV_PLAN_FEW; ++s)
+                if (q_lens[s] > 0)
+                    rows.add(masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < size ? q_lens[s] : size), (q_lens[s] + size - 1) / size * m->Hkv, true);
+            std::sort(rows.row, rows.row + rows.n, [](const auto &x, const auto &y) { return x.pages > y.pages; });
+            if (f == 2) (void)masked_part_pages(*m, rows, 32, true, (int64_t)(m->ws_floats / partial_floats(32, m->D)), &units);
+            else (void)masked_part_pairs(*m, rows, &groups);
+        }
+        if (units < groups && g_items == 0) form = 2;
+    }
     if (g_mask_form >= 0) form = total <= 1 << 16 ? g_mask_form : 1;
     g_last_mask_form = form;
     const int group = form == 0 ? 16 / m->g : (form == 2 ? tile : PKV_PREFILL_WAVES * tile);
@@ -2703,21 +2727,21 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
     PlanBuilder plan(batch, PKV_PLAN_FEW);
     if (form != 1) {
         d.cols = form == 0 ? 16 : 32;
-        // Partials of a launch's units, in the split-K workspace; arrivals are counted by sequence and kv head, so that only sequences of one group are cut.
-        const int64_t slots = (int64_t)(m->ws_floats / partial_floats(d.cols, m->D)) / m->Hkv;
+        // Partials of a launch's units, in the split-K workspace; arrivals are counted by sequence, group and kv head, so that only sequences of few groups are cut.
+        const int64_t slots = (int64_t)(m->ws_floats / partial_floats(d.cols, m->D));
         auto groups_of = [&](int s) { return (q_lens[s] + group - 1) / group; };
         for (int s0 = 0; s0 < batch;) {
             const int s1 = s0 + plan.per_launch < batch ? s0 + plan.per_launch : batch;
             MaskRows &rows = g_mask_rows;
             rows.n = rows.longest = 0;
             for (int s = s0; s < s1; ++s)
-                if (q_lens[s] > 0) rows.add(pages_of(s), groups_of(s) * m->Hkv, groups_of(s) == 1);
+                if (q_lens[s] > 0) rows.add(pages_of(s), groups_of(s) * m->Hkv, groups_of(s) <= PKV_MASK_GROUPS);
             std::sort(rows.row, rows.row + rows.n, [](const auto &a, const auto &b) { return a.pages > b.pages; });
-            int part = masked_part_pages(*m, rows, (most < group ? most : group) * m->g, form == 2);
-            auto parts_of = [&](int s) { return groups_of(s) == 1 && pages_of(s) > part ? (pages_of(s) + part - 1) / part : 1; };
+            int part = masked_part_pages(*m, rows, (most < group ? most : group) * m->g, form == 2, slots);
+            auto parts_of = [&](int s) { return groups_of(s) <= PKV_MASK_GROUPS && pages_of(s) > part ? (pages_of(s) + part - 1) / part : 1; };
             for (;; part += (part / 4 + 7) / 8 * 8) {
                 int64_t units = 0;
-                for (int s = s0; s < s1; ++s) units += (int64_t)groups_of(s) * parts_of(s);
+                for (int s = s0; s < s1; ++s) units += (int64_t)groups_of(s) * parts_of(s) * m->Hkv;
                 if (units <= slots || part >= rows.longest) break;
             }
             d.part_pages = (part / 2 + 7) / 8 * 8;

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d
     u.chunk = pu.rows;
     u.tokens = pu.rows - u.chunk0 < size ? pu.rows - u.chunk0 : size;
     u.first = pu.row + u.chunk0;
-    u.slot = u.seq * d.Hkv + u.kvh;                       // (a sequence that comes in parts has one group)
+    u.slot = (u.seq * PKV_MASK_GROUPS + group) * d.Hkv + u.kvh;       // (looked at where a sequence comes in parts: it has few groups then)
     const size_t floats = partial_floats(MC, D);
     u.partial = ((size_t)(unit - u.part) * d.Hkv + u.kvh) * floats;
     u.step = (size_t)d.Hkv * floats;
