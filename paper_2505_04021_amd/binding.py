@@ -591,24 +591,26 @@ class PrismKV:
         assert len(ql) == 4 * n
         return self.lib.prefill_attention_window(model, n, _at(q), ql, _at(ctx_lens), window, sinks, _at(out))
 
-    def _tree(self, ql, ctx_lens, sees):
+    def _tree(self, batch, tokens, ctx_lens, sees):
         """Words of a row of a tree's mask; 0, which the library refuses, where a tensor holds less than the call would read."""
-        tokens = _total(ql)
-        if sees.element_size() != 8 or sees.dim() != 2 or not sees.is_contiguous() or sees.shape[0] < tokens or 4 * ctx_lens.numel() < len(ql):
+        shape = sees.shape
+        if len(shape) != 2 or shape[0] < tokens or sees.element_size() != 8 or not sees.is_contiguous() or ctx_lens.numel() < batch:
             return 0
-        return sees.shape[1]
+        return shape[1]
 
     def qkv_append_tree_dev(self, model, q, k, v, q_lens, ctx_lens, sees, q_out, q_weight=None, k_weight=None, eps=1e-6, rotary=-1, before=None):
         """qkv_append_chunk_dev of drafted tokens; sees: device tensor, int64 (bits) [tokens][words].  Only enqueues."""
         ql = _i32(q_lens)
-        n, words = len(ql) // 4, self._tree(ql, ctx_lens, sees)
-        x = self._qkv(model, n, _total(ql), q_out, q, k, v, q_weight, k_weight, eps, rotary, before)
+        n, tokens = len(ql) // 4, _total(ql)
+        words = self._tree(n, tokens, ctx_lens, sees)
+        x = self._qkv(model, n, tokens, q_out, q, k, v, q_weight, k_weight, eps, rotary, before)
         return self.lib.qkv_append_tree(model, n, x, ql, _at(ctx_lens), _at(sees), words, q_out.data_ptr() if x else None)
 
     def tree_attention_dev(self, model, q, q_lens, ctx_lens, sees, out, window=0, sinks=0):
         """Drafted tokens over their contexts; sees as in qkv_append_tree_dev.  Only enqueues."""
         ql = _i32(q_lens)
-        return self.lib.tree_attention(model, len(ql) // 4, _at(q), ql, _at(ctx_lens), _at(sees), self._tree(ql, ctx_lens, sees), window, sinks, _at(out))
+        n = len(ql) // 4
+        return self.lib.tree_attention(model, n, _at(q), ql, _at(ctx_lens), _at(sees), self._tree(n, _total(ql), ctx_lens, sees), window, sinks, _at(out))
 
     def kv_keep_dev(self, model, q_lens, ctx_lens, kept, n_kept, new_lens=None):
         """Device tensors, int32: kept [tokens], n_kept and new_lens [B]; q_lens: list or host int32 array.  All layers; only enqueues."""

@@ -262,6 +262,9 @@ struct Rotary {
 };
 Rotary g_rotary[PKV_MAX_ROTARY];
 constexpr int64_t kQueryWaves = 4096;     // waves for queries that a launch of qkv_append_chunk has at least, where there are as many
+// The same of qkv_append_tree, where every wave counts its token's drafts before it can turn anything: us with 4096, 2048, 1024, 512 for 714 drafted tokens of
+// 32/8/128 11.4, 9.5, 9.4, 9.9, of 1700 of 16/4/128 12.4, 10.2, 9.4, 9.4, of 1663 into an e4m3 cache 16.3, 17.0, 14.8, 14.9; alike below 300 tokens.
+constexpr int64_t kTreeQueryWaves = 1024;
 
 // An angle as a fraction of a circle, to the nearest 2^-64 of one: the 53 bits of the angle times 128 of 1 / 2 pi, in integers.  A position of
 // 31 bits multiplies what is lost here, so that it has to be less than a double keeps: a fraction of 53 bits, as the quotient in doubles is, put angles at
@@ -1922,9 +1925,9 @@ static int fill_qkv(QkvArgs &a, const Model &m, const pkv_qkv &in, void *q_out) 
 
 // Query heads of a token per wave: few tokens come a wave for every 512 elements, many a wave each (its angles are worked out once).  Ragged prompts
 // of 4300 tokens of 32/8/128, us with 4, 8, 16 and 32 heads a wave 42.1, 31.0, 27.2, 26.8; of 2400 into an e4m3 cache 21.6, 15.8, 13.7, 14.1.
-static int wave_heads_for(const Model &m, int64_t tokens) {
+static int wave_heads_for(const Model &m, int64_t tokens, int64_t waves = kQueryWaves) {
     const int at_once = 512 / m.D, turns = (m.Hq + at_once - 1) / at_once;
-    int64_t n = turns * tokens / kQueryWaves;
+    int64_t n = turns * tokens / waves;
     n = n < 1 ? 1 : (n > turns ? turns : n);
     return (int)n * at_once;
 }
@@ -1981,7 +1984,7 @@ static int run_qkv_chunk(int model, int batch, const pkv_qkv *in, const int32_t 
         a.sees = sees;
         a.words = words;
     }
-    a.wave_heads = wave_heads_for(*m, total);
+    a.wave_heads = wave_heads_for(*m, total, tree ? kTreeQueryWaves : kQueryWaves);
     AttnDesc d{};
     fill_addressing(d, *m);
     d.batch = batch;

@@ -116,17 +116,18 @@ __global__ __launch_bounds__(64 * KEEP_WAVES) void k_kv_keep(const AttnDesc d, c
     const int row0 = (int)(plan.s[i].row & PKV_PLAN_ROWS), drafted = (int)(plan.s[i + 1].row & PKV_PLAN_ROWS) - row0;
     const int ctx = PKV_CONST(int32_t, d.ctx_lens)[seq], n = PKV_CONST(int32_t, n_kept)[seq], cap = PKV_CONST(int32_t, d.row_len)[seq] * PKV_T;
     kept += row0;
+    int at = lane < drafted ? kept[lane] : 0;             // (asked for with the lengths)
     const int base = ctx - drafted;
     bool fine = base >= 0 && ctx <= cap && n >= 0 && n <= drafted;
     int from = n;                                         // the first token that is not in its place already
     if (fine) {
+        int front = -1;
         for (int j0 = 0; j0 < n; j0 += 64) {
             const int j = j0 + lane;
-            int at = j, last = -1;
-            if (j < n) {
-                at = kept[j];
-                last = j > 0 ? kept[j - 1] : -1;
-            }
+            if (j0 > 0) at = j < n ? kept[j] : 0;
+            int last = __shfl_up(at, 1);
+            if (lane == 0) last = front;
+            front = __builtin_amdgcn_readlane(at, 63);
             if (__any(j < n && (at <= last || at >= drafted))) fine = false;
             const uint64_t moves = __ballot(j < n && at != j);
             if (moves && from == n) from = j0 + (int)__ffsll((long long)moves) - 1;
