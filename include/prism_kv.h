@@ -413,7 +413,8 @@ int prefill_attention_prefix(int model, int batch, const void *q, const int32_t 
  * Layers whose queries do not see all that is cached, and drafted tokens that are verified many at a time.  Everything not said
  * here is as in decode_attention_ex (with the library's table), prefill_attention and qkv_append_chunk: outputs dev fp32, fp32 accumulation, 16
  * significant bits of every probability on both cache types, zero rows where nothing is seen.  What a query does not see does
- * not reach it, whatever it holds, where none of the call's queries sees it.  Small calls keep partial sums in the split-K workspace, others in a
+ * not reach it, whatever it holds; an infinity or a NaN that it sees leaves it elements that are not finite (and costs a work-group that
+ * holds such a row a second walk).  Small calls keep partial sums in the split-K workspace, others in a
  * buffer of the model, made or enlarged when first needed (PKV_E_NOMEM while the stream is being captured: make the call once
  * before the capture): two of the attention calls of this section on one model must not overlap in time, nor one with a decode_attention* call
  * or a call behind shared prefixes.  Otherwise they only enqueue.

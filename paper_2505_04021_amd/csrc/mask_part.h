@@ -187,13 +187,16 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
         const int p = page0 + STEP * k;
         return below(walk.len - PKV_T * p) & (p + 1 < pe ? 0xffffffffu : 0xffffu);
     };
-    auto mask_scores = [&](float (*s)[8], int k) __attribute__((always_inline)) {
+    auto sees = [&](int c, int k) __attribute__((always_inline)) {    // of those, the ones that this lane's column of tile c sees
         const int x0 = PKV_T * (page0 + STEP * k);
+        uint32_t mine = seen_bits(x0, hi[c], lo[c], walk.sinks);
+        if constexpr (TREE) mine |= row_bits(mask_row[c], 2 * mk.words, x0 - base);
+        return mine & there(k);
+    };
+    auto mask_scores = [&](float (*s)[8], int k) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-            uint32_t mine = seen_bits(x0, hi[c], lo[c], walk.sinks);
-            if constexpr (TREE) mine |= row_bits(mask_row[c], 2 * mk.words, x0 - base);
-            mine = (mine & there(k)) >> (4 * G);
+            const uint32_t mine = sees(c, k) >> (4 * G);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                  // (a select, so that a NaN logit of an unseen token cannot leak)
                 if (!(mine >> i & 1u)) s[c][i] = -INFINITY;
@@ -291,6 +294,68 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
             if (masked) mask_v(r, k);
             products(r, ph, pl);
             load_v(k + 1);
+        }
+    }
+    // once more, if sums are not finite (mask_walk.h)
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int jt = 0; jt < TL::NV; ++jt) sum += (st[c].acc[jt][0] + st[c].acc[jt][1]) + (st[c].acc[jt][2] + st[c].acc[jt][3]);
+    if (__builtin_expect(__any(!is_finite(sum)), 0)) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+#pragma unroll
+            for (int jt = 0; jt < TL::NV; ++jt) st[c].acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            st[c].m = -INFINITY;
+            st[c].l = 0.f;
+        }
+#pragma unroll 1
+        for (int k = 0; k < n_pairs; ++k) {
+            if (k % 32 == 0) locate(k);
+            PairRegs<D, DT> r;
+            load(r.a.k, tiles(k, 0), 0);
+            load(r.b.k, tiles(k, 1), 0);
+            load(r.a.v, tiles(k, 0), TL::TILE_BYTES);
+            load(r.b.v, tiles(k, 1), TL::TILE_BYTES);
+            if (DT == PKV_E4M3) {
+                r.a.sk = scale_of(page_sk, k, 0);
+                r.a.sv = scale_of(page_sv, k, 0);
+                r.b.sk = scale_of(page_sk, k, 1);
+                r.b.sv = scale_of(page_sv, k, 1);
+            }
+            float s[NT][8];
+            scores(s, r);
+            mask_scores(s, k);
+            bf16x8 ph[NT], pl[NT];
+            u32x4 mine[NT];
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const uint32_t bits = sees(c, k) >> (4 * G);
+                mine[c] = mk4(halves_of(bits), halves_of(bits >> 2), halves_of(bits >> 16), halves_of(bits >> 18));
+                softmax_pair<D, DT>(st[c], s[c], r.a.sv, r.b.sv, ph[c], pl[c]);
+                ph[c] = as_bf16x8(__builtin_bit_cast(u32x4, ph[c]) & mine[c]);       // (a block's scale may be none, too)
+                pl[c] = as_bf16x8(__builtin_bit_cast(u32x4, pl[c]) & mine[c]);
+            }
+            mask_v(r, k);
+#pragma unroll
+            for (int jt = 0; jt < TL::NV; ++jt) {
+                const u32x2 va = v_half<D, DT>(r.a, jt), vb = v_half<D, DT>(r.b, jt);
+                const u32x4 off = mk4(strange_halves(va.x), strange_halves(va.y), strange_halves(vb.x), strange_halves(vb.y)) & kSpoil;
+#pragma unroll
+                for (int c = 0; c < NT; ++c) {
+                    st[c].acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(off), as_bf16x8(mine[c] & kSpoil), st[c].acc[jt], 0, 0, 0);
+                    st[c].acc[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(off), as_bf16x8(mine[c] & kMinusSpoil), st[c].acc[jt], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < TL::NL; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    r.a.v[j][i] = finite_only<DT>(r.a.v[j][i]);
+                    r.b.v[j][i] = finite_only<DT>(r.b.v[j][i]);
+                }
+            products(r, ph, pl);
         }
     }
 #pragma unroll

@@ -68,6 +68,23 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t four) {
     return (four & 1u ? 0xffu : 0u) | (four & 2u ? 0xff00u : 0u) | (four & 4u ? 0xff0000u : 0u) | (four & 8u ? 0xff000000u : 0u);
 }
 
+// Infinities and NaN in V.  A token that some columns of a tile see and others do not has the probability 0 in the others' products, and 0 * NaN spoils their sums.
+// So a wave whose sums are not all finite at its walk's end walks once more, with zeros for what is not finite in V; what sees such an element is
+// spoiled by finite factors: products of 2^127 where the element is not finite with +-2^127 where the column sees the token are infinities of both signs, and 0
+// elsewhere.  (Looking through V in every pair under masks, and this in the walk itself, took 1 to 10 % of all calls' time, and registers that there are not.)
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+// the halves of a word of bf16 values that are no finite ones, as masks
+__device__ __forceinline__ uint32_t strange_halves(uint32_t w) {
+    return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+// a word of V with zeros for what is not finite
+template <int DT>
+__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+    if constexpr (DT == PKV_BF16) return w & ~strange_halves(w);
+    else return w & ~((((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu);
+}
+constexpr uint32_t kSpoil = 0x7f007f00u, kMinusSpoil = 0xff00ff00u;  // two bf16 values, 2^127 and its negative
+
 constexpr int MASK_WORDS = 2 * PKV_TREE_WORDS;           // 32-bit words of a row of a tree's mask in LDS
 
 }  // namespace

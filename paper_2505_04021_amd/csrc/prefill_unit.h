@@ -234,26 +234,27 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
     uint32_t vr[TL::ND][2][2 * VW];
     const int unit = 8 * hi16 + (n & 7), half = (n >> 3) & 1;
     const uint8_t *v_lane = ring + PF_SLOTS * SLOT + h * 256 + (UNITS ? hi16 * 1024 + c16 * 16 : unit * 16 + half * 8);
+    auto v_words = [&](int k, const uint8_t *src) __attribute__((always_inline)) {
+        if constexpr (DT == PKV_BF16) {
+#pragma unroll
+            for (int dt = 0; dt < TL::ND; ++dt) {
+                const u32x2 a = *reinterpret_cast<const u32x2 *>(src + dt * 1024), b = *reinterpret_cast<const u32x2 *>(src + dt * 1024 + 512);
+                vr[dt][k][0] = a.x; vr[dt][k][1] = a.y; vr[dt][k][2] = b.x; vr[dt][k][3] = b.y;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                typedef uint32_t words __attribute__((ext_vector_type(TL::ND)));
+                const words a = *reinterpret_cast<const words *>(src + q * 512);
+#pragma unroll
+                for (int dt = 0; dt < TL::ND; ++dt) vr[dt][k][q] = a[dt];
+            }
+        }
+    };
     auto read_v = [&](int r) __attribute__((always_inline)) {
         const uint8_t *src = v_lane + (r & (PF_SLOTS - 1)) * SLOT;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if constexpr (DT == PKV_BF16) {
-#pragma unroll
-                for (int dt = 0; dt < TL::ND; ++dt) {
-                    const uint8_t *at = src + k * TL::BYTES + dt * 1024;
-                    const u32x2 a = *reinterpret_cast<const u32x2 *>(at), b = *reinterpret_cast<const u32x2 *>(at + 512);
-                    vr[dt][k][0] = a.x; vr[dt][k][1] = a.y; vr[dt][k][2] = b.x; vr[dt][k][3] = b.y;
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    typedef uint32_t words __attribute__((ext_vector_type(TL::ND)));
-                    const words a = *reinterpret_cast<const words *>(src + k * TL::BYTES + q * 512);
-#pragma unroll
-                    for (int dt = 0; dt < TL::ND; ++dt) vr[dt][k][q] = a[dt];
-                }
-            }
+        for (int k = 0; k < 2; ++k) v_words(k, src + k * TL::BYTES);
     };
     auto k_op = [&](int kk) __attribute__((always_inline)) {
         if constexpr (DT == PKV_BF16) return as_bf16x8(kr[kk]);
@@ -539,6 +540,76 @@ __device__ __forceinline__ void prefill_unit(const AttnDesc &d, const UNIT &u, i
             while (++r < plain);
         }
         for (; r < np; ++r) step();
+    }
+
+    if constexpr (UNIT::MASKED) {
+        // once more, if sums are not finite (mask_walk.h), from memory
+        float sum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < TL::ND; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) sum += (acc[dt][i] + acc[dt][i + 1]) + (acc[dt][i + 2] + acc[dt][i + 3]);
+        if (__builtin_expect(__any(!is_finite(sum)), 0)) {
+#pragma unroll
+            for (int dt = 0; dt < TL::ND; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+            m = PF_M0;
+            l = 0.f;
+            bar = kSumBar;
+            // (what the walk itself does not keep is worked out again: with 64-wide e4m3 heads one register more were one work-group a CU fewer)
+            int id = (int)threadIdx.x;
+            asm volatile("" : "+v"(id));
+            const int page_of = id >> 4 & 1, k_from = (id >> 5 & 1) * 256 + (id & 15) * 16;
+            const int v_from = (id >> 5 & 1) * 256 + (UNITS ? page_of * 1024 + (id & 15) * 16 : (8 * page_of + (id & 7)) * 16 + (id >> 3 & 1) * 8);
+#pragma unroll 1
+            for (int p = p_begin; p < p_end; ++p) {
+                if (!((32 * p < tile_lim) & takes(p))) continue;
+                const uint32_t ida = table_id(2 * p), idb = table_id(2 * p + 1);
+                const uint64_t k_at = (DT == PKV_E4M3 ? PKV_FP8_HEADER : 0) + (uint64_t)kvh * 2 * TL::BYTES;
+                const uint8_t *k_src = (page_of ? block_of(2 * p + 1, idb, k_at) : block_of(2 * p, ida, k_at)) + k_from;
+#pragma unroll
+                for (int u = 0; u < TL::NU; ++u) kr[u] = *reinterpret_cast<const u32x4 *>(k_src + u * 512);
+                if (DT == PKV_E4M3) {
+                    const float *ha = reinterpret_cast<const float *>(block_of(2 * p, ida, 0)), *hb = reinterpret_cast<const float *>(block_of(2 * p + 1, idb, 0));
+                    sca = ha[kvh] * d.scale_log2;
+                    scb = hb[kvh] * d.scale_log2;
+                    sva = ha[d.Hkv + kvh];
+                    svb = hb[d.Hkv + kvh];
+                }
+                scores();
+                args(p, true);
+                settle(p, true);
+                const uint32_t bits = seen(p);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pr[i] = unseen(bits, i) ? 0.f : pr[i] * (DT == PKV_BF16 ? 1.f : i < 8 ? sva : svb);     // (a block's scale may be none, too)
+                sva = svb = 1.f;
+                probabilities();
+                if (LOW) low_halves();
+                __builtin_amdgcn_sched_barrier(0);                   // (no more registers than the walk takes)
+                v_words(0, block_of(2 * p, ida, k_at + TL::BYTES) + v_from);
+                v_words(1, block_of(2 * p + 1, idb, k_at + TL::BYTES) + v_from);
+                blank_v(p);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t b = bits >> (16 * k);
+                    const u32x4 mine = mk4(halves_of(b), halves_of(b >> 2), halves_of(b >> 8), halves_of(b >> 10));
+#pragma unroll
+                    for (int dt = 0; dt < TL::ND; ++dt) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        u32x4 off = __builtin_bit_cast(u32x4, v_op(dt, k));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) off[i] = strange_halves(off[i]) & kSpoil;
+                        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(off), as_bf16x8(mine & kSpoil), acc[dt], 0, 0, 0);
+                        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(off), as_bf16x8(mine & kMinusSpoil), acc[dt], 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 2 * VW; ++i) vr[dt][k][i] = finite_only<DT>(vr[dt][k][i]);
+                    }
+                }
+                accumulate(ph);
+                if (LOW) accumulate(pl);
+            }
+        }
     }
 
     l += __shfl_xor(l, 32);
