@@ -196,21 +196,27 @@ hipError_t pkv_launch_window(const AttnDesc &d, const MaskArgs &mk, hipStream_t 
 
 hipError_t pkv_launch_masked(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, hipStream_t s) {
     if (plan.s[plan.n_seqs].unit == 0) return hipSuccess;
-    const auto few = few_of(plan);
-    if (d.cols <= 16) {
-        if (tree) launch<1, true>(d, mk, few, s);
-        else launch<1, false>(d, mk, few, s);
-    } else {
-        if (tree) launch<2, true>(d, mk, few, s);
-        else launch<2, false>(d, mk, few, s);
-    }
+    auto with = [&](const auto &p) {
+        if (d.cols <= 16) {
+            if (tree) launch<1, true>(d, mk, p, s);
+            else launch<1, false>(d, mk, p, s);
+        } else {
+            if (tree) launch<2, true>(d, mk, p, s);
+            else launch<2, false>(d, mk, p, s);
+        }
+    };
+    if (plan.n_seqs <= PKV_PLAN_FEW) with(few_of(plan));
+    else with(plan);
     return hipGetLastError();
 }
 
 hipError_t pkv_launch_masked_wide(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, int split_groups, hipStream_t s) {
     if (plan.s[plan.n_seqs].unit == 0) return hipSuccess;
-    const auto few = few_of(plan);
-    if (tree) launch_wide<true>(d, mk, few, split_groups, s);
-    else launch_wide<false>(d, mk, few, split_groups, s);
+    auto with = [&](const auto &p) {
+        if (tree) launch_wide<true>(d, mk, p, split_groups, s);
+        else launch_wide<false>(d, mk, p, split_groups, s);
+    };
+    if (plan.n_seqs <= PKV_PLAN_FEW) with(few_of(plan));
+    else with(plan);
     return hipGetLastError();
 }
