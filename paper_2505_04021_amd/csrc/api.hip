@@ -2515,11 +2515,13 @@ struct MaskRows {
     struct Row {
         int pages, units;                         // of the walk; units (groups x kv heads) of so many
         bool cut;                                 // may come in parts
+        int count;                                // rows that this one stands for
     } row[PKV_MAX_SEQS];
     int n = 0, longest = 0;
     void add(int pages, int units, bool cut) {
         row[n].pages = pages;
         row[n].units = units;
+        row[n].count = 1;
         row[n++].cut = cut;
         if (pages > longest) longest = pages;
     }
@@ -2528,7 +2530,7 @@ struct MaskRows {
     void order() {
         constexpr int kFew = 64, kClasses = 16 * 31;
         if (n > kFew) {
-            static struct { int64_t pages, units; } all[2][kClasses];
+            static struct { int64_t pages, units; int count; } all[2][kClasses];
             memset(all, 0, sizeof all);
             for (int i = 0; i < n; ++i) {
                 const float x = (float)(row[i].pages > 1 ? row[i].pages : 1);
@@ -2537,12 +2539,13 @@ struct MaskRows {
                 auto &to = all[row[i].cut][(bits >> 19) - (127u << 4)];
                 to.pages += (int64_t)row[i].pages * row[i].units;
                 to.units += row[i].units;
+                to.count++;
             }
             n = 0;
             for (int c = kClasses - 1; c >= 0; --c)
                 for (int cut = 0; cut < 2; ++cut)
                     if (all[cut][c].units > 0)
-                        row[n++] = Row{(int)((all[cut][c].pages + all[cut][c].units - 1) / all[cut][c].units), (int)all[cut][c].units, cut != 0};
+                        row[n++] = Row{(int)((all[cut][c].pages + all[cut][c].units - 1) / all[cut][c].units), (int)all[cut][c].units, cut != 0, all[cut][c].count};
         } else
             std::sort(row, row + n, [](const Row &x, const Row &y) { return x.pages > y.pages; });
     }
@@ -2559,17 +2562,25 @@ static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two
     constexpr int kPlaces = 768;
     const double tau = two_tiles ? (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.27 : 0.72) : (m.D == 128 ? 1.09 : 0.83))
                                  : (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.02 : 0.44) : (m.D == 128 ? 0.55 : 0.39));
-    const double step = (double)m.D * (m.dtype == PKV_BF16 ? 4 : 2) * 128 / 7.5e6;          // the memory's time for eight pages
+    double pages_read = 0.0, pages_held = 1e-9;
+    for (int i = 0; i < rows.n; ++i) {
+        pages_read += (double)rows.row[i].pages * rows.row[i].units;
+        pages_held += (double)rows.row[i].pages * rows.row[i].count * m.Hkv;
+    }
+    const double groups = pages_read > pages_held ? pages_read / pages_held : 1.0;
+    // the memory's time for eight pages; those that several groups of a row read take half of it again for each
+    const double step = (double)m.D * (m.dtype == PKV_BF16 ? 4 : 2) * 128 / 7.5e6 * (0.5 + 0.5 / groups);
     auto with = [&](int n) {                      // what a step takes where n CUs are at work
         const double shared = n * step, more = tau > shared ? tau : shared, x = (tau > shared ? shared : tau) / more;
         return more * (1.0 + 0.19 * x * x * x * x);
     };
     double load[(int)kSmallCUs + 1] = {}, total = 0.0, longest = 0.0;
+    const double per_part = 1.0 / part;
     int most = 1;
     int64_t wgs = 0, cut = 0;
     for (int i = 0; i < rows.n; ++i) {
-        const int pages = rows.row[i].pages, parts = rows.row[i].cut && pages > part ? (pages + part - 1) / part : 1;
-        const double steps = (double)((pages + parts * 8 - 1) / (parts * 8));
+        const int pages = rows.row[i].pages, parts = rows.row[i].cut && pages > part ? (int)((pages + part - 0.5) * per_part) : 1;
+        const double steps = (double)(int)((pages + parts * 8 - 0.5) / (parts * 8.0));
         const int64_t n = (int64_t)parts * rows.row[i].units;
         most = most > parts ? most : parts;
         longest = longest > steps ? longest : steps;
@@ -2724,32 +2735,41 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
     MaskArgs mk = mask_args(window, sinks);
     mk.sees = sees;
     mk.words = words;
-    // Few columns a kv head: units of 16 or 32, whose four waves walk different pages; many: groups of 128, whose waves walk the same pages with 32 each.  Between,
-    // what either is estimated to take decides: units of 32 want no join launch and start sooner, but every 32 columns read the context for themselves.  Us, units
-    // of 32 and groups: 40 columns of 16/8/128 e4m3, 16 x 500 tokens 15.4, 22.4; 64 columns, 64 x 3125 tokens of 16/4/128 bf16 182, 115; 96, 4 x 4000 of 4/4/128 24.5, 25.2.
+    // Up to 16 columns a kv head (query tokens x heads) are one unit of 16, whose four waves walk different pages.  More come as several such units, as units of 32,
+    // each of which reads the context for itself, or as groups of 128, whose waves walk the same pages with 32 columns each: what they are estimated to take decides, for
+    // units of 32 with the eighth more that they take.  Us as units of 16, of 32 and as groups: 40 columns of 16/8/128 e4m3, 16 x 500 tokens 11.2, 12.6, 19.5; 96
+    // of 4/4/128, 4 x 4000 22.3, 21.6, 22.9; 64 of 16/4/128, 64 x 3125 185, 132, 80.  Of 1000 random trees of 17 to 128 columns the choice takes what the best of the three
+    // takes to 1 %, one in twenty 7 to 10 % more (always units of 32 up to 32 columns: 15 %, 47 %).
     int most = 0;
     for (int s = 0; s < batch; ++s) most = most > q_lens[s] ? most : q_lens[s];
     const int tile = PKV_PREFILL_COLS / PKV_PREFILL_WAVES / m->g;
+    auto group_of = [&](int f) { return f == 0 ? 16 / m->g : (f == 2 ? tile : PKV_PREFILL_WAVES * tile); };
     PlanBuilder plan(batch);
-    int form = most * m->g <= 16 ? 0 : (most <= tile ? 2 : 1);
-    if (form == 1 && most <= PKV_MASK_GROUPS * tile) {
-        MaskRows &rows = g_mask_rows;
-        double units = 0.0, groups = 0.0;
-        for (int f : {2, 1}) {
-            const int size = f == 2 ? tile : PKV_PREFILL_WAVES * tile;
+    int form = most <= group_of(0) ? 0 : 1;
+    if (form == 1 && most <= group_of(1) && g_items == 0) {
+        double best = 1e30;
+        for (int f : {0, 2, 1}) {
+            const int size = group_of(f);
+            if (f != 1 && most > PKV_MASK_GROUPS * size) continue;
+            MaskRows &rows = g_mask_rows;
             rows.n = rows.longest = 0;
             for (int s = 0; s < batch && s < plan.per_launch; ++s)
                 if (q_lens[s] > 0)
                     rows.add(masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < size ? q_lens[s] : size), (q_lens[s] + size - 1) / size * m->Hkv, true);
             rows.order();
-            if (f == 2) (void)masked_part_pages(*m, rows, 32, true, (int64_t)(m->ws_floats / partial_floats(32, m->D)), &units);
-            else (void)masked_part_pairs(*m, rows, &groups);
+            double us;
+            if (f == 1) (void)masked_part_pairs(*m, rows, &us);
+            else (void)masked_part_pages(*m, rows, (most < size ? most : size) * m->g, f == 2, (int64_t)(m->ws_floats / partial_floats(f == 2 ? 32 : 16, m->D)), &us);
+            if (f == 2) us *= 1.12;
+            if (us < best) {
+                best = us;
+                form = f;
+            }
         }
-        if (units < groups && g_items == 0) form = 2;
     }
     if (g_mask_form >= 0) form = total <= 1 << 16 ? g_mask_form : 1;
     g_last_mask_form = form;
-    const int group = form == 0 ? 16 / m->g : (form == 2 ? tile : PKV_PREFILL_WAVES * tile);
+    const int group = group_of(form);
     auto pages_of = [&](int s) { return masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < group ? q_lens[s] : group); };
     if (form != 1) {
         d.cols = form == 0 ? 16 : 32;

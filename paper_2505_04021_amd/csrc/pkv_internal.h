@@ -167,7 +167,7 @@ struct QkvArgs {
 
 // What queries see of their contexts where that is not all up to their own token.
 #define PKV_TREE_WORDS 4                // 64-bit words of a row of a drafted tree's mask at most
-#define PKV_MASK_GROUPS 4               // groups of 16 or 32 columns of a sequence that comes in parts at most
+#define PKV_MASK_GROUPS 8               // groups of 16 or 32 columns of a sequence that comes in parts at most
 #define PKV_NO_WINDOW (1 << 28)         // (contexts end at 2^24 tokens)
 struct MaskArgs {
     int32_t window, sinks;
