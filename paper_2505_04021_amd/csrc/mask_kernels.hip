@@ -5,7 +5,9 @@
 
 namespace {
 
-// The decode step: a work-group per part of a (sequence, kv head).
+// The decode step: a work-group per part of a (sequence, kv head).  Bound by memory: 64 windows of 1024 tokens and 4 sinks of 32/8/128, 271 MB, 43 us (6.3 TB/s; a large
+// read comes at 6.6); 96 of 4096 and 19 of 64/8/128 e4m3, 814 MB, 131 us.  Four of up to 132 tokens of 8/2/64 4.2 us, dependent trips.  (decode_attention, which
+// reads all of the first call's 6000-token contexts, moves six times as much.)
 template <int D, int DT>
 __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_window_decode(const AttnDesc d, const MaskArgs mk) {
     __shared__ __align__(16) float s_acc[kMaskSums<1>];
@@ -35,7 +37,11 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_window_decode(const Att
     masked_part<D, DT, 1, false>(d, mk, u, s_acc, s_m, s_l, nullptr, &s_arrived);
 }
 
-// Chunks and drafted trees: a unit of the plan is a group of 16 NT / g query tokens, or one of the parts of what it sees.
+// Chunks and drafted trees: a unit of the plan is a group of 16 NT / g query tokens, or one of the parts of what it sees.  16 columns of 64 x 1000 tokens of 32/8/128,
+// 314 MB: 61 us (5.1 TB/s; the longest row is four times the mean: 56 with the best cut of all); 28 columns, 48 windows of 1024 of 32/8/128 e4m3, 107 MB: 26.  A unit's
+// four waves walk different pages, so that each page is read by one of them; many columns are multiplied by every unit for itself (26 drafts of 32 sequences of
+// 32/8/128, 104 columns behind 1500 tokens, 136 as units of 16, 62 as groups).  Of 32 columns: K of the next pair asked for behind the scores, V behind the products, in the
+// registers that are free (two pairs in turn, as units of 16 have them, spill).
 template <int D, int DT, int NT, bool TREE, int SEQS>
 __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d, const MaskArgs mk, const PlanOf<SEQS> plan) {
     constexpr int MC = kMaskCols<NT>;
@@ -64,7 +70,12 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d
     masked_part<D, DT, NT, TREE>(d, mk, u, s_acc, s_m, s_l, s_mask, &s_arrived);
 }
 
-// Groups of up to 128 columns (prefill_unit.h): a group of query tokens, four waves with 32 columns each, or one of the parts of what it sees.
+// Groups of up to 128 columns (prefill_unit.h): a group of query tokens, four waves with 32 columns each, or one of the parts of what it sees.  Bound by the matrix pipes
+// with 128-wide heads: three large trees of 64/8/128 behind 20000 tokens 150 us, 1.0 PFLOP/s executed (a plain product reaches 1.15 to 1.27); whole prompts of
+// 6 x 1500 tokens of 32/8/128 with windows of 512 103, 86 GFLOP and 148 MB of outputs (260 as units of 16): a walk has 17 pairs of pages and costs as much as six more until its
+// first one and behind its last one.  By vector instructions with 64-wide heads and e4m3: chunks of 5 x 512 tokens of 32/8/64 e4m3 with windows of 2000 90 us, 25.9 million,
+// some 42 us of issue, by 560 work-groups on 256 CUs (a third of the chunk cut in three: 85, all of it: 102).
+// A wave leaves out pairs in front of its own queries' windows and behind their last token, and takes masks only where its own columns differ.
 template <bool TREE>
 struct MaskedGroup {
     static constexpr bool CAUSAL = false, LEVELS = true, SHARED = false, MASKED = true;

@@ -493,8 +493,8 @@ __device__ __forceinline__ int depth_of(const uint64_t *row, int words, int n) {
     return seen > 0 ? seen - 1 : 0;
 }
 
-//
-// TREE: drafted tokens, whose positions go by how many drafted tokens each sees (its row of a.sees).
+// TREE: drafted tokens, whose positions go by how many drafted tokens each sees (its row of a.sees).  714 of 32/8/128, 18 MB: 9.4 us, two thirds of the waves' time
+// waiting for dependent trips (the same tokens as a chunk 10.4).
 template <int D, int DT, int SEQS, bool TREE>
 __global__ __launch_bounds__(64 * QKV_WAVES, 4) void k_qkv_append_chunk(const AttnDesc d, const QkvArgs a, const PlanOf<SEQS> plan) {
     constexpr int E = DT == PKV_BF16 ? 2 : 1;
