@@ -166,3 +166,70 @@ def test_largest_and_smallest(gpu, form):  # noqa: F811
         M.check(out.cpu().double().numpy(), q, lambda s: rows.kv[s], n, lambda s: M.window_seen(lens[s], n[s], 1, 0))
     assert gpu.device_errors() == 0
     rows.c.close()
+
+
+@pytest.mark.parametrize("n", [200, 1000])
+def test_many_sequences(gpu, n):  # noqa: F811
+    """More sequences than a launch's shorter and longer plan hold: drafts appended, attended to, kept; no rotation, so that keys are what came in."""
+    hq, hkv, d = 4, 1, 64
+    rng = np.random.default_rng(n)
+    base, new = rng.integers(0, 40, n).tolist(), rng.integers(0, 7, n).tolist()
+    c = P.Cache(gpu, hq, hkv, d, BF16, [x + 7 for x in base], frames=40)
+    masks = [M.random_tree(rng, x, 0.5) for x in new]
+    total, ctx = sum(new), [a + b for a, b in zip(base, new)]
+    kv = []
+    for s, x in enumerate(base):
+        raw = gen.seq_kv((86, s), max(x, 1), hkv, d, BF16, 16)
+        c.fill(s, raw, x)
+        kv.append([P.f64(raw[y][:x]) for y in ("k", "v")])
+    q, k, v = (gen.queries((87, i), total, h, d) for i, h in enumerate((hq, hkv, hkv)))
+    at = np.cumsum([0] + new)
+    for s in range(n):
+        kv[s] = [np.concatenate([old, P.f64(x[at[s]:at[s + 1]])]) for old, x in zip(kv[s], (k, v))]
+    sees, lens = M.words_of(sum(masks, []), 1), P.i32(ctx)
+    q_out, out = torch.zeros((total, hq, d), dtype=torch.int16, device="cuda"), torch.full((total, hq, d), float("nan"), device="cuda")
+    assert gpu.qkv_append_tree_dev(c.m, P.dev(q), P.dev(k), P.dev(v), new, lens, sees, q_out) == total
+    assert gpu.tree_attention_dev(c.m, q_out, new, lens, sees, out) == 0
+    torch.cuda.synchronize()
+    assert np.array_equal(P.host(q_out).view(np.int16), q.view(np.int16))
+    M.check(out.cpu().double().numpy(), q, lambda s: kv[s], new, lambda s: M.tree_seen(ctx[s], masks[s], 0, 0))
+    paths = [M.path_of(x[int(rng.integers(len(x)))]) if x else [] for x in masks]
+    packed = sum([p + [0] * (m - len(p)) for p, m in zip(paths, new)], [])
+    left = P.i32([0] * n)
+    assert gpu.kv_keep_dev(c.m, new, lens, P.i32(packed), P.i32([len(p) for p in paths]), left) == n
+    torch.cuda.synchronize()
+    assert left.tolist() == [b + len(p) for b, p in zip(base, paths)]
+    for s in rng.choice(n, 60, replace=False).tolist() + [0, n - 1]:
+        rows = list(range(base[s])) + [base[s] + j for j in paths[s]]
+        if rows:
+            for got, want in zip(c.read(s, 0, len(rows)), kv[s]):
+                assert np.array_equal(got, want[rows]), s
+    assert gpu.device_errors() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_blocks_beyond_4_gib(gpu, form, dtype):  # noqa: F811
+    """Rows whose blocks lie all over a pool of 5 GiB: read under windows and masks, moved together."""
+    hq, hkv, d, n, lens = 16, 4, 128, [5, 20], [400, 300]
+    rows = Rows(gpu, hq, hkv, d, dtype, lens, frames=5120)
+    c, rng = rows.c, np.random.default_rng(8)
+    masks = [M.random_tree(rng, x, 0.5) for x in n]
+    ctx, q = P.i32(lens), gen.queries((88,), sum(n), hq, d)
+    out = [torch.full((x, hq, d), float("nan"), device="cuda") for x in (2, sum(n), sum(n))]
+    assert gpu.decode_attention_window_dev(c.m, P.dev(q[:2]), ctx, 150, 4, out[0]) == 0
+    assert gpu.prefill_attention_window_dev(c.m, P.dev(q), n, ctx, 150, 4, out[1]) == 0
+    assert gpu.tree_attention_dev(c.m, P.dev(q), n, ctx, M.words_of(sum(masks, []), 1), out[2]) == 0
+    got, row = [x.cpu().double().numpy() for x in out], lambda s: rows.kv[s]
+    M.check(got[0], q, row, [1, 1], lambda s: M.window_seen(lens[s], 1, 150, 4))
+    M.check(got[1], q, row, n, lambda s: M.window_seen(lens[s], n[s], 150, 4))
+    M.check(got[2], q, row, n, lambda s: M.tree_seen(lens[s], masks[s], 0, 0))
+    before = [c.read(s, 0, x) for s, x in enumerate(lens)]
+    assert gpu.kv_keep_dev(c.m, n, ctx, P.i32([0, 3, 0, 0, 0] + [2, 19] + [0] * 18), P.i32([2, 2])) == 2
+    for s, stay in enumerate(([395, 398], [282, 299])):
+        # (moved into an e4m3 block: within half a step of its values, and of bf16 on the way, under a scale that may have grown: e4m3 2^-4, bf16 2^-8 relative, or
+        # half the lowest step, 2^-10, of the scale, which no value here has above 2^-3)
+        for x, y in zip(c.read(s, lens[s] - n[s], 2), before[s]):
+            assert np.all(np.abs(x - y[stay]) <= (0.0 if dtype == BF16 else 1.0) * (np.abs(y[stay]) * (2.0 ** -4 + 2.0 ** -7) + 2.0 ** -13)), s
+    assert gpu.device_errors() == 0
+    c.close()
