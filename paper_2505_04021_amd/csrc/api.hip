@@ -2558,7 +2558,8 @@ struct MaskRows {
 // them tau or n times the memory's time for its bytes.  Parts cost their join, work-groups beyond the places on the chip a start of their own.
 // The figures are fitted to 6200 launches (900 random calls, 24 to 1000 pages a part): the choice takes 2.5 % more than the best of all in the geometric mean,
 // one in twenty 11 % or more; cut into 512 shares' worth of pages 8.8 % and 30 %, never cut 20 % and 71 %.
-static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int part, int64_t slots) {
+// An estimate that cannot come below `limit` is not worked out.
+static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int part, int64_t slots, double limit) {
     constexpr int kPlaces = 768;
     const double tau = two_tiles ? (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.27 : 0.72) : (m.D == 128 ? 1.09 : 0.83))
                                  : (m.dtype == PKV_BF16 ? (m.D == 128 ? 1.02 : 0.44) : (m.D == 128 ? 0.55 : 0.39));
@@ -2574,34 +2575,42 @@ static double masked_us(const Model &m, const MaskRows &rows, int cols, bool two
         const double shared = n * step, more = tau > shared ? tau : shared, x = (tau > shared ? shared : tau) / more;
         return more * (1.0 + 0.19 * x * x * x * x);
     };
-    double load[(int)kSmallCUs + 1] = {}, total = 0.0, longest = 0.0;
+    double total = 0.0, longest = 0.0;
     const double per_part = 1.0 / part;
+    static double steps[PKV_MAX_SEQS];                    // of a work-group of each row
+    static int units[PKV_MAX_SEQS];                       // work-groups of each row
     int most = 1;
     int64_t wgs = 0, cut = 0;
     for (int i = 0; i < rows.n; ++i) {
         const int pages = rows.row[i].pages, parts = rows.row[i].cut && pages > part ? (int)((pages + part - 0.5) * per_part) : 1;
-        const double steps = (double)(int)((pages + parts * 8 - 0.5) / (parts * 8.0));
-        const int64_t n = (int64_t)parts * rows.row[i].units;
+        steps[i] = (double)(int)((pages + parts * 8 - 0.5) / (parts * 8.0));
+        units[i] = parts * rows.row[i].units;
         most = most > parts ? most : parts;
-        longest = longest > steps ? longest : steps;
-        total += (double)n * steps;
-        for (int64_t k = wgs; k < wgs + n && k < kPlaces; ++k) load[k % kSmallCUs] += steps;
-        wgs += n;
-        if (parts > 1) cut += n;
+        longest = longest > steps[i] ? longest : steps[i];
+        total += units[i] * steps[i];
+        wgs += units[i];
+        if (parts > 1) cut += units[i];
     }
     if (most > 1 && wgs > slots) return 1e30;
+    const double full = with((int)kSmallCUs);
     double us = 5.4 + 4.3e-6 * (double)cut * cols * m.D;
-    if (wgs > kPlaces) us += total / kSmallCUs * with((int)kSmallCUs) + 0.5 * longest * tau;       // work-groups go where there is room
-    else
+    if (us + total / kSmallCUs * full >= limit) return 1e30;           // (a step with n CUs at work takes at least n 256ths of one with all)
+    if (wgs > kPlaces) us += total / kSmallCUs * full + 0.5 * longest * tau;       // work-groups go where there is room
+    else {
+        double load[(int)kSmallCUs + 1] = {};
+        int at = 0;
+        for (int i = 0; i < rows.n; ++i)
+            for (int k = 0; k < units[i]; ++k, ++at) load[at % kSmallCUs] += steps[i];
         for (int i = 0; i < kSmallCUs; ++i)
             if (load[i] != load[i + 1]) us += (load[i] - load[i + 1]) * with(i + 1);
+    }
     if (wgs > kSmallWorkGroups) us += (two_tiles ? 0.72 : 0.06) * (double)(wgs - kSmallWorkGroups) / kSmallCUs;
     if (most > 1) us += 0.96 + 0.12 * (most < 8 ? most : 8) + 0.14 * (most > 8 ? most - 8 : 0);
     return us;
 }
 
 // Pages of a part: of some lengths the one that is estimated to be the best.  `slots`: work-groups whose partials the workspace takes.
-static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int64_t slots, double *estimate = nullptr) {
+static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, bool two_tiles, int64_t slots, double *estimate = nullptr, double limit = 1e30) {
     const int least = ((rows.longest + kSmallMaxParts - 1) / kSmallMaxParts + 7) / 8 * 8;
     if (g_items > 0) {
         double pages = 0.0;
@@ -2611,11 +2620,11 @@ static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, boo
     }
     int best = rows.longest > 8 ? rows.longest : 8;
     if (best <= kMaskPart[0] && !estimate) return best;
-    double best_us = masked_us(m, rows, cols, two_tiles, best, slots);
+    double best_us = masked_us(m, rows, cols, two_tiles, best, slots, limit);
     for (int part : kMaskPart) {
         if (part >= rows.longest) break;
         if (part < least) continue;
-        const double us = masked_us(m, rows, cols, two_tiles, part, slots);
+        const double us = masked_us(m, rows, cols, two_tiles, part, slots, best_us < limit ? best_us : limit);
         if (us < best_us) {
             best_us = us;
             best = part;
@@ -2628,45 +2637,50 @@ static int masked_part_pages(const Model &m, const MaskRows &rows, int cols, boo
 // The same for groups of 128 columns and parts of `pairs` page pairs (0: uncut).  A work-group takes t1 us a pair by itself and t2 a pair beside another one on its CU, and
 // every one takes kGroupPairs pairs besides its own; beyond two to a CU they go where there is room.  Parts' sums are written and read once, and joined by a launch of
 // their own.  Fitted to 3100 launches (350 random calls): the choice takes 1.7 % more than the best, one in twenty 7.6 % or more (prefill_part_pairs 2.7 and 13.2).
-static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs) {
+static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs, double limit) {
     const bool bf16 = m.dtype == PKV_BF16, wide = m.D == 128;
     const double t1 = wide ? (bf16 ? 0.60 : 0.70) : (bf16 ? 0.42 : 0.52), t2 = wide ? (bf16 ? 0.40 : 0.49) : (bf16 ? 0.28 : 0.34);
     constexpr double kGroupPairs = 5.7;
-    double load[2][(int)kSmallCUs] = {}, total = 0.0, longest = 0.0, bytes = 0.0;
+    double total = 0.0, longest = 0.0, bytes = 0.0;
+    static double length[PKV_MAX_SEQS];                   // of a work-group of each row
+    static int units[PKV_MAX_SEQS];                       // work-groups of each row
     int64_t wgs = 0, cut = 0;
     for (int i = 0; i < rows.n; ++i) {
         bytes += (double)rows.row[i].units * rows.row[i].pages * (m.D * (bf16 ? 64 : 32));
         const int all = (rows.row[i].pages + 1) / 2, parts = prefill_parts(rows.row[i].pages, pairs);
-        const double len = (all + parts - 1) / parts + kGroupPairs;
-        const int64_t n = (int64_t)parts * rows.row[i].units;
-        longest = longest > len ? longest : len;
-        total += (double)n * len;
-        for (int64_t k = wgs; k < wgs + n && k < kSmallWorkGroups; ++k) load[k / kSmallCUs][k % kSmallCUs] = len;
-        wgs += n;
-        if (parts > 1) cut += n;
+        length[i] = (all + parts - 1) / parts + kGroupPairs;
+        units[i] = parts * rows.row[i].units;
+        longest = longest > length[i] ? longest : length[i];
+        total += units[i] * length[i];
+        wgs += units[i];
+        if (parts > 1) cut += units[i];
     }
+    const double joins = cut > 0 ? 4.4 + 1.2e-6 * (double)cut * PKV_PREFILL_COLS * (m.D + 4) : 0.0;
+    if (5.3 + longest * t1 + joins >= limit) return 1e30;
     double us = longest * t1;
     if (wgs > kSmallWorkGroups) {
         const double even = total / kSmallCUs * t2 + 0.585 * us;
         us = even > us ? even : us;
     } else if (wgs > kSmallCUs) {
+        double load[2][(int)kSmallCUs] = {};
+        int at = 0;
+        for (int i = 0; i < rows.n; ++i)
+            for (int k = 0; k < units[i]; ++k, ++at) load[at / kSmallCUs][at % kSmallCUs] = length[i];
         for (int i = 0; i < kSmallCUs; ++i) {
             const double a = load[0][i], b = load[1][i], both = 2.0 * (a < b ? a : b) * t2 + fabs(a - b) * t1;
             us = us > both ? us : both;
         }
     }
     const double memory = bytes / 6.8e6, more = us > memory ? us : memory, x = (us > memory ? memory : us) / (more > 0.0 ? more : 1.0);
-    us = 5.3 + more * (1.0 + 0.19 * x * x * x * x);
-    if (cut > 0) us += 4.4 + 1.2e-6 * (double)cut * PKV_PREFILL_COLS * (m.D + 4);
-    return us;
+    return 5.3 + more * (1.0 + 0.19 * x * x * x * x) + joins;
 }
 
-static double masked_part_pairs(const Model &m, const MaskRows &rows, double *estimate = nullptr) {
+static double masked_part_pairs(const Model &m, const MaskRows &rows, double *estimate = nullptr, double limit = 1e30) {
     if (g_items > 0) return (double)g_items;
-    double best = 0.0, best_us = masked_wide_us(m, rows, 0.0);
+    double best = 0.0, best_us = masked_wide_us(m, rows, 0.0, limit);
     for (int pages : kMaskPart) {
         if (pages >= rows.longest) break;
-        const double us = masked_wide_us(m, rows, pages * 0.5);
+        const double us = masked_wide_us(m, rows, pages * 0.5, best_us < limit ? best_us : limit);
         if (us < best_us) {
             best_us = us;
             best = pages * 0.5;
@@ -2758,8 +2772,8 @@ static int run_masked(int model, int batch, const void *q, const int32_t *q_lens
                     rows.add(masked_pages(m->row_len[s], mk.window, mk.sinks, q_lens[s] < size ? q_lens[s] : size), (q_lens[s] + size - 1) / size * m->Hkv, true);
             rows.order();
             double us;
-            if (f == 1) (void)masked_part_pairs(*m, rows, &us);
-            else (void)masked_part_pages(*m, rows, (most < size ? most : size) * m->g, f == 2, (int64_t)(m->ws_floats / partial_floats(f == 2 ? 32 : 16, m->D)), &us);
+            if (f == 1) (void)masked_part_pairs(*m, rows, &us, best);
+            else (void)masked_part_pages(*m, rows, (most < size ? most : size) * m->g, f == 2, (int64_t)(m->ws_floats / partial_floats(f == 2 ? 32 : 16, m->D)), &us, f == 2 ? best / 1.12 : best);
             if (f == 2) us *= 1.12;
             if (us < best) {
                 best = us;
