@@ -78,7 +78,9 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, 2) void k_masked(const AttnDesc d
 // A wave leaves out pairs in front of its own queries' windows and behind their last token, and takes masks only where its own columns differ.
 template <bool TREE>
 struct MaskedGroup {
-    static constexpr bool CAUSAL = false, LEVELS = true, SHARED = false, MASKED = true;
+    // (levels of priority, us with and without: windows of 1024 in 8 x 512 tokens of 32/8/128 136, 124; of 4096 in 4 x 512 of 64/8/128 415, 404; of 2048 in 8 x 512 of
+    // 32/8/128 e4m3 181, 186; 60 drafts for 16 sequences behind 4000 tokens of 32/8/128 127, 130, e4m3 138, 141)
+    static constexpr bool CAUSAL = false, LEVELS = TREE, SHARED = false, MASKED = true;
     const MaskArgs &mk;
     int seq, q0, ntok, part, parts, slot;
     const int32_t *own;

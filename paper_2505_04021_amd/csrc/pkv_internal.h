@@ -279,8 +279,8 @@ hipError_t pkv_launch_prefill_prefixed(const AttnDesc &d, const ChunkPlan &plan,
 hipError_t pkv_launch_prefix(const AttnDesc &d, const PrefixPlan &plan, hipStream_t s);
 // small calls of the same, by whole contexts; d as for a launch of the small decode kernel, at most PKV_PLAN_FEW sequences
 hipError_t pkv_launch_prefixed_small(const AttnDesc &d, const SharedRows &shared, hipStream_t s);
-// attention with windows and sinks: a decode step (d.parts, d.part_pages as for a small launch); chunks and drafted trees, at most PKV_PLAN_FEW
-// sequences, by units of 16 columns (d.cols = g) or of PKV_PREFILL_COLS (d.cols and split_groups as in pkv_launch_prefill)
+// attention with windows and sinks: a decode step (d.parts, d.part_pages as for a small launch); chunks and drafted trees, by units of 16 or 32
+// columns (d.cols) or by groups of PKV_PREFILL_COLS (d.cols and split_groups as in pkv_launch_prefill)
 hipError_t pkv_launch_window(const AttnDesc &d, const MaskArgs &mk, hipStream_t s);
 hipError_t pkv_launch_masked(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, hipStream_t s);
 hipError_t pkv_launch_masked_wide(const AttnDesc &d, const MaskArgs &mk, const ChunkPlan &plan, bool tree, int split_groups, hipStream_t s);
