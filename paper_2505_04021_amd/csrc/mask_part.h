@@ -58,6 +58,16 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
             qf[c][j] = *reinterpret_cast<bf16x8 *>(&v);
         }
     }
+    // rows of a tree's mask are asked for here and looked at behind the first pages' loads (on the device, us, looked at here and so: five drafts of four chats of
+    // 8/2/64 5.4, 5.2; seven of 48 sequences of 32/8/128 e4m3 27.7, 26.7)
+    uint64_t bits[NT][PKV_TREE_WORDS];
+    if constexpr (TREE) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int i = 0; i < PKV_TREE_WORDS; ++i)      // (a column that stands for no query has the first token's)
+                bits[c][i] = mk.sees[(size_t)(u.first + tok[c]) * mk.words + (i < mk.words ? i : mk.words - 1)];
+    }
     int ctx = PKV_CONST(int32_t, d.ctx_lens)[u.seq], cap = PKV_CONST(int32_t, d.row_len)[u.seq];
     asm volatile("" : "+s"(ctx), "+s"(cap));              // both at once
     cap *= PKV_T;
@@ -68,20 +78,6 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
     if constexpr (TREE) {
         base = ctx - u.chunk;
         L = base < 0 ? 0 : (ctx < cap ? ctx : cap);
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            // (a column that stands for no query has the first token's)
-            const uint64_t *bits = mk.sees + (size_t)(u.first + tok[c]) * mk.words;
-            const int seen = seen_drafts(bits, mk.words, u.chunk);
-            mask_row[c] = s_mask + (w * MC + tok[c]) * MASK_WORDS;
-            for (int i = 0; i < mk.words; ++i) {
-                const uint64_t x = bits[i];
-                mask_row[c][2 * i] = (uint32_t)x;
-                mask_row[c][2 * i + 1] = (uint32_t)(x >> 32);
-            }
-            hi[c] = base;
-            lo[c] = base + (seen > 0 ? seen : 1) - window;
-        }
         lo_first = base + 1 - window;
         lo_last = base + u.chunk - window;
         hi_first = base;
@@ -100,12 +96,33 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
     }
     const Walk walk = walk_of(L, lo_first, lo_last, hi_first, mk.sinks);
     const int shift = walk.skip * PKV_T;
-#pragma unroll
-    for (int c = 0; c < NT; ++c) {
-        hi[c] -= shift;
-        lo[c] -= shift;
-    }
     base -= shift;
+    if constexpr (!TREE) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            hi[c] -= shift;
+            lo[c] -= shift;
+        }
+    }
+    auto tree_masks = [&]() __attribute__((always_inline)) {
+        if constexpr (TREE) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                int seen = 0;
+                mask_row[c] = s_mask + (w * MC + tok[c]) * MASK_WORDS;
+#pragma unroll
+                for (int i = 0; i < PKV_TREE_WORDS; ++i)
+                    if (i < mk.words) {
+                        const int left = u.chunk - 64 * i;
+                        seen += __popcll(bits[c][i] & (left >= 64 ? ~0ull : (left <= 0 ? 0ull : (1ull << left) - 1ull)));
+                        mask_row[c][2 * i] = (uint32_t)bits[c][i];
+                        mask_row[c][2 * i + 1] = (uint32_t)(bits[c][i] >> 32);
+                    }
+                hi[c] = base;
+                lo[c] = base + (seen > 0 ? seen : 1) - window;
+            }
+        }
+    };
     const int n_pages = walk.pages(), max_parts = u.parts;
     constexpr int STEP = 2 * SMALL_WAVES;
     // as many parts of equal length as the host asked for, but none shorter than u.size
@@ -253,6 +270,7 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
             PairRegs<D, DT> ring[2];
             locate(0);
             load_pair(ring[0], 0);
+            tree_masks();
             int k = 0;
             if (n_pairs > 1) {
                 do {
@@ -281,6 +299,7 @@ __device__ __forceinline__ void masked_part(const AttnDesc &d, const MaskArgs &m
         locate(0);
         load_k(0);
         load_v(0);
+        tree_masks();
         for (int k = 0; k < n_pairs; ++k) {
             if (k + 1 - pair0 >= 32) locate(k + 1);
             const bool masked = pair_is_masked(k);
