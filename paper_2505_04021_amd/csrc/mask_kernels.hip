@@ -167,6 +167,9 @@ __global__ __launch_bounds__(64 * PF_WAVES, 2) void k_masked_wide(const AttnDesc
     prefill_unit<D, DT, MEET, true>(d, MaskedGroup<TREE>(gi, d, mk, group, lanes.find(plan, (uint32_t)group).rows, rows), kvh, ring);
 }
 
+// On e4m3 caches the waves of a group of drafts meet once in two pairs of pages, of a chunk once in four.  Us, met in two and in four: 60 drafts for 16 sequences
+// behind 4000 tokens of 32/8/64 84.1, 86.8, of 32/8/128 135.7, 137.0; 32 drafts of 64 behind windows of 1024 58.5, 59.8; windows of 2048 in chunks of 8 x 512 tokens of
+// 32/8/128 190, 186, of 8000 in 2 x 512 230, 226.
 template <bool TREE, int SEQS>
 void launch_wide(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan, int split_groups, hipStream_t s) {
     const dim3 grid(plan.s[plan.n_seqs].unit * (unsigned)d.Hkv), wg(64 * PF_WAVES);
@@ -174,8 +177,9 @@ void launch_wide(const AttnDesc &d, const MaskArgs &mk, const PlanOf<SEQS> &plan
         if (d.D == 128) hipLaunchKernelGGL((k_masked_wide<128, PKV_BF16, 2, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
         else hipLaunchKernelGGL((k_masked_wide<64, PKV_BF16, 2, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
     } else {
-        if (d.D == 128) hipLaunchKernelGGL((k_masked_wide<128, PKV_E4M3, 4, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
-        else hipLaunchKernelGGL((k_masked_wide<64, PKV_E4M3, 4, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        constexpr int MEET = TREE ? 2 : 4;
+        if (d.D == 128) hipLaunchKernelGGL((k_masked_wide<128, PKV_E4M3, MEET, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
+        else hipLaunchKernelGGL((k_masked_wide<64, PKV_E4M3, MEET, TREE, SEQS>), grid, wg, 0, s, d, mk, plan);
     }
     if (split_groups > 0) launch_merge(d, plan, split_groups, s);
 }

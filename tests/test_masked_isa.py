@@ -30,7 +30,7 @@ def test_units(asm):
 
 
 def test_groups(asm):
-    for d, dtype, meet in ((128, 0, 2), (64, 0, 2), (128, 1, 4), (64, 1, 4)):
+    for d, dtype, meet in ((128, 0, 2), (64, 0, 2), (128, 1, 2), (64, 1, 2), (128, 1, 4), (64, 1, 4)):
         name = f"13k_masked_wideILi{d}ELi{dtype}ELi{meet}E"
         insn, labels = check(asm, name)
         if d == 64:
