@@ -31,7 +31,8 @@ int pkv_stream_read_probe(size_t bytes, size_t granule_bytes, int iters, double 
 /* Measurement / test knobs of the attention work split: `items` = work items (waves)
  * per launch, `min_share` = smallest number of pages a wave may be given; 0 selects
  * the automatic value of either (items: what the chip holds at once; min_share: an
- * eighth of a mean row, within 4..16 pages). */
+ * eighth of a mean row, within 4..16 pages).  Calls with windows or drafted trees are cut into about `items` work-groups, as far as rows are long
+ * enough and the workspace has room; their form is then the one that the number of columns alone would give. */
 int pkv_set_split(int items, int min_share);
 /* What a (sequence, kv head) segment is taken to cost besides its pages when the pages
  * are cut into shares, in pages (0..256; -1 = the default).  A wave whose share holds

@@ -2676,7 +2676,11 @@ static double masked_wide_us(const Model &m, const MaskRows &rows, double pairs,
 }
 
 static double masked_part_pairs(const Model &m, const MaskRows &rows, double *estimate = nullptr, double limit = 1e30) {
-    if (g_items > 0) return (double)g_items;
+    if (g_items > 0) {
+        double pages = 0.0;
+        for (int i = 0; i < rows.n; ++i) pages += (double)rows.row[i].pages * rows.row[i].units;
+        return pages / g_items * 0.5 > 8.0 ? pages / g_items * 0.5 : 8.0;
+    }
     double best = 0.0, best_us = masked_wide_us(m, rows, 0.0, limit);
     for (int pages : kMaskPart) {
         if (pages >= rows.longest) break;

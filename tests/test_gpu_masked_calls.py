@@ -233,3 +233,28 @@ def test_blocks_beyond_4_gib(gpu, form, dtype):  # noqa: F811
             assert np.all(np.abs(x - y[stay]) <= (0.0 if dtype == BF16 else 1.0) * (np.abs(y[stay]) * (2.0 ** -4 + 2.0 ** -7) + 2.0 ** -13)), s
     assert gpu.device_errors() == 0
     c.close()
+
+
+@pytest.mark.parametrize("items", [1, 64, 700, 100000])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(16, 4, 128, BF16), (4, 4, 64, E4M3)])
+def test_cut_as_asked(gpu, form, hq, hkv, d, dtype, items):  # noqa: F811
+    """Any number of parts: one, a few, more than the workspace has room for."""
+    n, lens = [3, 50, 1, 8], [5000, 1200, 40, 8]
+    rows = Rows(gpu, hq, hkv, d, dtype, lens, frames=100)
+    rng, ctx = np.random.default_rng(items), P.i32(lens)
+    masks = [M.random_tree(rng, x, 0.5) for x in n]
+    q, row = gen.queries((89, d), sum(n), hq, d), lambda s: rows.kv[s]
+    out = [torch.full((x, hq, d), float("nan"), device="cuda") for x in (4, sum(n), sum(n))]
+    assert gpu.set_split(items, 0) == 0
+    try:
+        assert gpu.decode_attention_window_dev(rows.c.m, P.dev(q[:4]), ctx, 3000, 20, out[0]) == 0
+        assert gpu.prefill_attention_window_dev(rows.c.m, P.dev(q), n, ctx, 3000, 20, out[1]) == 0
+        assert gpu.tree_attention_dev(rows.c.m, P.dev(q), n, ctx, M.words_of(sum(masks, []), 1), out[2]) == 0
+    finally:
+        gpu.set_split(0, 0)
+    got = [x.cpu().double().numpy() for x in out]
+    M.check(got[0], q, row, [1] * 4, lambda s: M.window_seen(lens[s], 1, 3000, 20))
+    M.check(got[1], q, row, n, lambda s: M.window_seen(lens[s], n[s], 3000, 20))
+    M.check(got[2], q, row, n, lambda s: M.tree_seen(lens[s], masks[s], 0, 0))
+    assert gpu.device_errors() == 0
+    rows.c.close()
